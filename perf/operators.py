@@ -1,0 +1,462 @@
+"""Measured cases of the steps that follow a composed prefill: the rows of a
+decode or extend step over requests whose KV sits in request pages.
+
+A case is an operator and a batch layout:
+
+  op        "append"  query/key norms per head, RoPE and the page write of the
+                      step's rows, from one fused projection's output
+            "attn"    attention of the step's rows over the pages, under a
+                      sliding window with sinks (window 0: every earlier key)
+            "attn4"   the same over pages held in 4 bits (e2m1 codes, one
+                      power-of-two scale for each 32 dims of a token's head)
+            "pack4"   a request's bf16 pages into 4-bit pages and back
+  kv        "bf16" or "f32" (activations alike); the 4-bit operators take bf16
+  hq, hkv, d            query heads, KV heads, head dim
+  page                  tokens per KV page
+  requests              requests in the batch
+  len_lo .. len_hi      keys of a request once the step's rows are in, log-uniform
+  rows_lo .. rows_hi    rows of a request, log-uniform, at most its keys
+  rows      "tail"      the last positions of the request (decode, extension)
+            "spread"    positions anywhere in it (recompute windows and text
+                        of a composed prompt)
+  window, sinks         attention only
+  k_pre                 append: the normalised keys before RoPE are wanted too
+                        (the form a unit cache keeps)
+  layout                seed of the lengths, positions and page order
+
+The layout follows from the case; the values follow from the seed.
+"""
+from __future__ import annotations
+
+import math
+import random
+from types import SimpleNamespace
+
+import torch
+
+own = False
+if own:
+    import paper_2609_32999_amd as P
+
+THETA = 500000.0
+EPS = 1e-6
+_DT = {"f32": torch.float32, "bf16": torch.bfloat16}
+_L8B = dict(kv="bf16", hq=32, hkv=8, d=128, page=16, rows="tail", window=0, sinks=0, k_pre=False)
+# magnitudes of the e2m1 codes 0 .. 7; bit 3 is the sign
+_E2M1 = [0.0, 0.5, 1.0, 1.5, 2.0, 3.0, 4.0, 6.0]
+
+
+def listed():
+    return [
+        # one token of one request: the smallest call, all launch and latency
+        dict(name="append_one", op="append", **_L8B, requests=1, len_lo=5216, len_hi=5216,
+             rows_lo=1, rows_hi=1, layout=1),
+        # the computed rows of a RAG batch; their keys go to the unit cache too
+        dict(name="append_prefill", op="append", **{**_L8B, "k_pre": True, "rows": "spread"},
+             requests=8, len_lo=5216, len_hi=5216, rows_lo=1500, rows_hi=2000, layout=2),
+        # the fp32 reference configuration: 4 heads of 64
+        dict(name="append_f32", op="append", **{**_L8B, "kv": "f32", "hq": 4, "hkv": 4, "d": 64,
+             "rows": "spread"}, requests=1, len_lo=272, len_hi=272, rows_lo=152, rows_hi=152,
+             layout=3),
+        # decode of one request under a window: the latency of a token
+        dict(name="window_one", op="attn", **{**_L8B, "window": 1024, "sinks": 4}, requests=1,
+             len_lo=5216, len_hi=5216, rows_lo=1, rows_hi=1, layout=4),
+        # a decode batch of agents with ragged histories, windowed layer
+        dict(name="window_batch", op="attn", **{**_L8B, "window": 4096, "sinks": 4}, requests=64,
+             len_lo=1000, len_hi=16000, rows_lo=1, rows_hi=1, layout=5),
+        # a decode batch on a full-attention layer of 64 query heads, long prompts
+        dict(name="full_batch", op="attn", **{**_L8B, "hq": 64}, requests=16, len_lo=8192,
+             len_hi=33000, rows_lo=1, rows_hi=1, layout=6),
+        # a long prompt's chunk through a windowed layer (the largest case)
+        dict(name="window_prefill", op="attn", **{**_L8B, "window": 4096, "sinks": 64},
+             requests=2, len_lo=12288, len_hi=12288, rows_lo=8192, rows_hi=8192, layout=7),
+        # the fp32 reference configuration, ragged
+        dict(name="window_f32", op="attn", **{**_L8B, "kv": "f32", "hq": 4, "hkv": 4, "d": 64,
+             "rows": "spread", "window": 100, "sinks": 3}, requests=1, len_lo=272, len_hi=272,
+             rows_lo=152, rows_hi=152, layout=8),
+        # one request decoding over a 33,000-token prompt in 4 bits
+        dict(name="four_bit_one", op="attn4", **_L8B, requests=1, len_lo=33000, len_hi=33000,
+             rows_lo=1, rows_hi=1, layout=9),
+        # a decode batch over 4-bit pages
+        dict(name="four_bit_batch", op="attn4", **_L8B, requests=32, len_lo=8192, len_hi=32768,
+             rows_lo=1, rows_hi=1, layout=10),
+        # a few more turns of text over 4-bit pages, windowed
+        dict(name="four_bit_extend", op="attn4", **{**_L8B, "window": 2048, "sinks": 4},
+             requests=4, len_lo=4000, len_hi=9000, rows_lo=60, rows_hi=400, layout=11),
+        # a RAG batch's request pages into 4 bits and back
+        dict(name="four_bit_pack", op="pack4", **_L8B, requests=8, len_lo=5216, len_hi=5216,
+             rows_lo=1, rows_hi=1, layout=12),
+    ]
+
+
+def _log_int(rng, lo, hi):
+    return int(round(math.exp(rng.uniform(math.log(lo), math.log(hi)))))
+
+
+def _layout(c):
+    """Per request: keys, the rows' positions (ascending) and page ids."""
+    rng = random.Random(c["layout"])
+    lens, rows = [], []
+    for _ in range(c["requests"]):
+        n = _log_int(rng, c["len_lo"], c["len_hi"])
+        t = min(n, _log_int(rng, c["rows_lo"], c["rows_hi"]))
+        lens.append(n)
+        if c["rows"] == "tail":
+            rows.append(list(range(n - t, n)))
+        else:
+            rows.append(sorted(rng.sample(range(n - 1), t - 1)) + [n - 1])
+    pages = [-(-n // c["page"]) for n in lens]
+    total = sum(pages) + 3          # a few pages nobody uses
+    ids = list(range(total))
+    rng.shuffle(ids)
+    tables, at = [], 0
+    for n in pages:
+        tables.append(ids[at:at + n])
+        at += n
+    return lens, rows, tables, total
+
+
+def _spans(c, p):
+    """Visible keys of a row at position p: sinks, then the window."""
+    lo = max(0, p - c["window"] + 1) if c["window"] else 0
+    return min(c["sinks"], lo), p + 1 - lo
+
+
+def work(case):
+    c = case
+    lens, rows, tables, total = _layout(c)
+    e = 4 if c["kv"] == "f32" else 2
+    T, d, hq, hkv = sum(len(r) for r in rows), c["d"], c["hq"], c["hkv"]
+    if c["op"] == "append":
+        head = T * (hq + 2 * hkv) * d * e
+        return {"bytes": 2 * head + T * hkv * d * e * c["k_pre"] + 4 * T * d + 2 * d * e,
+                "flops": 10 * T * (hq + hkv) * d}
+    if c["op"] == "pack4":
+        n = sum(lens) * hkv * d * 2
+        return {"bytes": 2 * n * 2 + 2 * n * 17 // 32, "flops": 6 * n}
+    keys = seen = 0
+    for r in rows:
+        top = -1                    # keys up to here are counted
+        sinks = 0
+        for p in r:
+            s, w = _spans(c, p)
+            keys += s + w
+            sinks = max(sinks, s)
+            a = max(p + 1 - w, top + 1)
+            seen += p + 1 - a
+            if top < 0:
+                first = p + 1 - w
+            top = p
+        seen += min(sinks, first)
+    kv_bytes = 2 * seen * hkv * d * e if c["op"] == "attn" else 2 * seen * hkv * (d // 2 + d // 32)
+    return {"bytes": kv_bytes + 2 * T * hq * d * e + 4 * T * hq, "flops": 4 * d * hq * keys}
+
+
+def _cost(c):
+    w = work(c)
+    return max(w["bytes"] / 5e12, w["flops"] / 8e14)
+
+
+def draw(rng):
+    """A case of the same ranges, at most the largest listed one's work."""
+    while True:
+        op = rng.choice(["append", "attn", "attn", "attn4", "attn4", "pack4"])
+        c = dict(_L8B, op=op, layout=rng.randrange(1 << 20))
+        if op in ("append", "attn") and rng.random() < 0.2:
+            c["kv"], c["d"] = "f32", rng.choice([64, 128])
+            g, c["hkv"] = rng.choice([(1, 4), (4, 2), (2, 4), (3, 2)])
+            c["requests"], top, most = rng.randint(1, 3), 1500, 200
+        else:
+            g, c["hkv"] = rng.choice([(4, 8), (4, 8), (8, 8), (8, 4), (2, 8), (1, 8), (5, 8), (16, 2)])
+            c["requests"], top, most = _log_int(rng, 1, 64), 33000, 4000
+            c["page"] = rng.choice([16, 16, 16, 32, 64])
+        c["hq"] = g * c["hkv"]
+        c["len_hi"] = _log_int(rng, 20, top)
+        c["len_lo"] = rng.randint(max(1, c["len_hi"] // 4), c["len_hi"])
+        if rng.random() < 0.4:
+            c["rows_hi"] = _log_int(rng, 2, most)
+            c["rows"] = rng.choice(["tail", "tail", "spread"])
+        else:
+            c["rows_hi"] = 1
+        c["rows_lo"] = rng.randint(1, c["rows_hi"])
+        if op in ("attn", "attn4") and rng.random() < 0.6:
+            c["window"] = _log_int(rng, 16, 8192)
+            c["sinks"] = rng.choice([0, 1, 4, 16, 64, 100])
+        c["k_pre"] = op == "append" and rng.random() < 0.5
+        scores = c["requests"] * c["rows_hi"] * c["len_hi"] * c["hq"]
+        cache = c["requests"] * c["len_hi"] * c["hkv"] * c["d"]
+        if scores <= 2e9 and cache <= 1.1e9 and _cost(c) <= max(_cost(x) for x in listed()):
+            return c
+
+
+def prepare(case, seed):
+    c = case
+    lens, rows, tables, total = _layout(c)
+    dt, dev = _DT[c["kv"]], "cuda"
+    gen = torch.Generator(dev).manual_seed(seed * 7919 + 13)
+
+    def rand(*shape, dtype=dt):
+        return torch.randn(shape, generator=gen, device=dev, dtype=torch.float32).to(dtype)
+
+    hq, hkv, d, page = c["hq"], c["hkv"], c["d"], c["page"]
+    T = sum(len(r) for r in rows)
+    most_rows, most_pages = max(len(r) for r in rows), max(len(t) for t in tables)
+    # rows of a request, padded with its first; pages likewise
+    pick, at = [], 0
+    for r in rows:
+        pick.append([at + min(i, len(r) - 1) for i in range(most_rows)])
+        at += len(r)
+    s = SimpleNamespace(
+        c=c, T=T, total=total,
+        pos=torch.tensor([p for r in rows for p in r], device=dev),
+        req=torch.tensor([i for i, r in enumerate(rows) for _ in r], device=dev),
+        slot=torch.tensor([p % page for r in rows for p in r], device=dev),
+        page=torch.tensor([t[p // page] for r, t in zip(rows, tables) for p in r], device=dev),
+        at=torch.tensor([i for r in rows for i in range(len(r))], device=dev),
+        pick=torch.tensor(pick, device=dev),
+        table=torch.tensor([t + t[:1] * (most_pages - len(t)) for t in tables], device=dev),
+        used=torch.tensor([x for t in tables for x in t], device=dev))
+    shape = (total, hkv, page, d)
+    if c["op"] == "append":
+        s.qkv = rand(T, (hq + 2 * hkv) * d)
+        s.wq = (1 + 0.1 * rand(d, dtype=torch.float32)).to(dt)
+        s.wk = (1 + 0.1 * rand(d, dtype=torch.float32)).to(dt)
+        s.req_k, s.req_v = rand(*shape), rand(*shape)
+        s.q_out = torch.empty(T, hq, d, dtype=dt, device=dev)
+        s.k_hat = torch.empty(T, hkv, d, dtype=dt, device=dev) if c["k_pre"] else None
+    elif c["op"] == "pack4":
+        s.req_k, s.req_v = rand(*shape), rand(*shape)
+    else:
+        # queries that prefer some keys, as trained ones do: scores spread over a few units
+        s.q = (1.5 * rand(T, hq, d, dtype=torch.float32)).to(dt)
+        s.out = torch.empty(T, hq, d, dtype=dt, device=dev)
+        s.lse = torch.empty(T, hq, dtype=torch.float32, device=dev)
+        if c["op"] == "attn":
+            s.req_k, s.req_v = rand(*shape), rand(*shape)
+    if c["op"] == "attn4":
+        s.req_k, s.req_v = (torch.randint(0, 256, (*shape[:3], d // 2), generator=gen, device=dev,
+                                          dtype=torch.uint8) for _ in range(2))
+        s.scale = torch.randint(124, 128, (total, 2, hkv, page, d // 32), generator=gen,
+                                device=dev, dtype=torch.uint8)
+    if c["op"] == "pack4":
+        s.codes = torch.zeros(2, total, hkv, page, d // 2, device=dev, dtype=torch.uint8)
+        s.scale = torch.zeros(total, 2, hkv, page, d // 32, device=dev, dtype=torch.uint8)
+        s.back_k, s.back_v = torch.zeros_like(s.req_k), torch.zeros_like(s.req_v)
+        # slots that hold a key
+        s.live = torch.zeros(total, page, dtype=torch.bool, device=dev)
+        for n, t in zip(lens, tables):
+            s.live[t] = True
+            if n % page:
+                s.live[t[-1], n % page:] = False
+    if own:
+        kv = "e2m1" if c["op"].endswith("4") else c["kv"]
+        m = P.make_model(hq, hkv, d, page, kv, c["kv"], THETA, 65536)
+        n = P.tsr_rope_table_bytes(m)
+        s.rope = torch.empty(n // 4, device=dev)
+        P.tsr_rope_table_init(m, s.rope, n, torch.cuda.current_stream())
+        batch = P.StepBatch([SimpleNamespace(kv_len=n, n_rows=len(r), positions=r, row_lo=None,
+                                             block_table=t)
+                             for n, r, t in zip(lens, rows, tables)])
+        opt = dict(window=c["window"], n_sinks=c["sinks"])
+        n = P.tsr_step_workspace_size(m, batch, total, **opt)
+        s.ws = torch.empty(n, dtype=torch.uint8, device=dev)
+        s.step = P.tsr_step_create(m, batch, total, s.rope, s.ws, n, torch.cuda.current_stream(),
+                                   **opt)
+    return s
+
+
+# ------------------------------------------------------------ plain forms
+def _rotate(x, pos):
+    """RoPE of x [T][H][d] (half-split pairs) at pos [T]; angles in 64 bits."""
+    h = x.shape[-1] // 2
+    inv = THETA ** (-torch.arange(h, device=x.device, dtype=torch.float64) / h)
+    a = (pos.double()[:, None] * inv)[:, None]
+    cs, sn = a.cos().to(x.dtype), a.sin().to(x.dtype)
+    lo, hi = x[..., :h], x[..., h:]
+    return torch.cat([lo * cs - hi * sn, hi * cs + lo * sn], -1)
+
+
+def _norm(x, w):
+    return x * torch.rsqrt((x * x).mean(-1, keepdim=True) + EPS) * w
+
+
+def _heads(s):
+    c = s.c
+    return s.qkv.view(s.T, c["hq"] + 2 * c["hkv"], c["d"]).split([c["hq"], c["hkv"], c["hkv"]], 1)
+
+
+def _plain_append(s):
+    q, k, v = _heads(s)
+    s.q_out.copy_(_rotate(_norm(q.float(), s.wq.float()), s.pos))
+    k_hat = _norm(k.float(), s.wk.float()).to(k.dtype)    # the form a cache keeps
+    s.req_k[s.page, :, s.slot] = _rotate(k_hat.float(), s.pos).to(k.dtype)
+    s.req_v[s.page, :, s.slot] = v
+    if s.k_hat is not None:
+        s.k_hat.copy_(k_hat)
+
+
+def _values(codes, scale):
+    """What 4-bit pages stand for: codes [..][d/2] (dim 2i in the low half),
+    scale [..][d/32] (power of two, exponent + 127)."""
+    grid = torch.tensor(_E2M1 + [-x for x in _E2M1], device=codes.device)
+    x = torch.stack([grid[(codes & 15).long()], grid[(codes >> 4).long()]], -1).flatten(-2)
+    s = torch.exp2(scale.float() - 127)
+    return (x.view(*s.shape, 32) * s[..., None]).flatten(-2)
+
+
+def _plain_attn(s):
+    c = s.c
+    hkv, g, d = c["hkv"], c["hq"] // c["hkv"], c["d"]
+    k, v = s.req_k[s.table], s.req_v[s.table]               # [R][pages][hkv][page][..]
+    if c["op"] == "attn4":
+        k, v = _values(k, s.scale[s.table, 0]), _values(v, s.scale[s.table, 1])
+    R = k.shape[0]
+    k, v = (x.float().transpose(1, 2).reshape(R, hkv, -1, d) for x in (k, v))
+    q = s.q.float()[s.pick].view(R, -1, hkv, g, d).permute(0, 2, 3, 1, 4)     # [R][hkv][g][n][d]
+    n = q.shape[3]
+    w = torch.matmul(q.reshape(R, hkv, g * n, d), k.transpose(2, 3).contiguous())
+    w = w.view(R, hkv, g, n, -1).mul_(1 / math.sqrt(d))
+    p = s.pos[s.pick][..., None]                            # [R][n][1]
+    j = torch.arange(k.shape[2], device=k.device)
+    seen = j <= p
+    if c["window"]:
+        seen &= (j > p - c["window"]) | (j < c["sinks"])
+    w.masked_fill_(~seen[:, None, None], -math.inf)
+    m = w.amax(-1, keepdim=True)
+    w.sub_(m).exp_()
+    z = w.sum(-1, keepdim=True)
+    o = torch.matmul(w.view(R, hkv, g * n, -1), v).view(R, hkv, g, n, d) / z
+    o = o.permute(0, 3, 1, 2, 4).reshape(R, n, -1, d)
+    lse = (m + z.log()).squeeze(-1).permute(0, 3, 1, 2).reshape(R, n, -1)
+    s.out.copy_(o[s.req, s.at])
+    s.lse.copy_(lse[s.req, s.at])
+
+
+def _plain_pack(x):
+    """bf16 values -> the values their 4-bit form stands for: for each 32 dims
+    the smallest power of two s with max |x| <= 6 s (1 for zeros), magnitudes
+    to the nearest of the grid, ties to the even code."""
+    b = x.float().view(*x.shape[:-1], -1, 32)
+    m, e = torch.frexp(b.abs().amax(-1, keepdim=True))
+    e = torch.where(m == 0, 0, torch.where(m <= 0.75, e - 3, e - 2))
+    y = torch.ldexp(b, -e)
+    a = y.abs()
+    step = torch.where(a < 2, 0.5, torch.where(a < 4, 1.0, 2.0))
+    return torch.ldexp(torch.copysign((a / step).round() * step, y), e).view(x.shape)
+
+
+def _result(s):
+    if s.c["op"] == "append":
+        r = dict(q=s.q_out, k=s.req_k, v=s.req_v)
+        return r if s.k_hat is None else dict(r, k_pre=s.k_hat)
+    if s.c["op"] == "pack4":
+        return dict(k=s.back_k, v=s.back_v)
+    return dict(out=s.out, lse=s.lse)
+
+
+def run(s):
+    op, c = s.c["op"], s.c
+    if own:
+        stream = torch.cuda.current_stream()
+        if op == "append":
+            q, k, v = _heads(s)
+            row = s.qkv.stride(0)
+            P.tsr_step_append(s.step, q, k, v, s.req_k, s.req_v, None, s.q_out, k_pre=s.k_hat,
+                              norm=P.make_qk_norm(s.wq, s.wk, EPS), q_stride=row, k_stride=row,
+                              v_stride=row, stream=stream)
+        elif op == "pack4":
+            P.tsr_step_pack_kv(s.step, s.req_k, s.req_v, s.codes[0], s.codes[1], s.scale, stream)
+            P.tsr_step_unpack_kv(s.step, s.codes[0], s.codes[1], s.scale, s.back_k, s.back_v,
+                                 stream)
+        else:
+            P.tsr_step_attn(s.step, s.q, s.req_k, s.req_v, s.scale if op == "attn4" else None,
+                            s.out, s.lse, stream)
+    elif op == "append":
+        _plain_append(s)
+    elif op == "pack4":
+        live = s.live[:, None, :, None]
+        s.back_k.copy_(torch.where(live, _plain_pack(s.req_k), s.back_k))
+        s.back_v.copy_(torch.where(live, _plain_pack(s.req_v), s.back_v))
+    else:
+        _plain_attn(s)
+    return _result(s)
+
+
+# ------------------------------------------------------ 64-bit definitions
+def exact(case, seed):
+    s = prepare(case, seed)
+    c = case
+    hq, hkv, d, page = c["hq"], c["hkv"], c["d"], c["page"]
+    if c["op"] == "append":
+        x = s.qkv.double().view(s.T, hq + 2 * hkv, d)
+
+        def unit(y, w):
+            return y * w.double() / (y.pow(2).sum(-1, keepdim=True) / d + EPS).sqrt()
+
+        ang = torch.outer(s.pos.double(), torch.pow(
+            torch.tensor(THETA, dtype=torch.float64, device=x.device),
+            -2.0 * torch.arange(d // 2, device=x.device, dtype=torch.float64) / d))
+        turn = torch.polar(torch.ones_like(ang), ang)[:, None]
+
+        def spin(y):
+            z = torch.complex(y[..., :d // 2], y[..., d // 2:]) * turn
+            return torch.cat([z.real, z.imag], -1)
+
+        kh = unit(x[:, hq:hq + hkv], s.wk)
+        k, v = s.req_k.double(), s.req_v.double()
+        # the keys rotate as the cache keeps them, in the activations' type
+        k[s.page, :, s.slot] = spin(kh.to(_DT[c["kv"]]).double())
+        v[s.page, :, s.slot] = x[:, hq + hkv:]
+        r = dict(q=spin(unit(x[:, :hq], s.wq)), k=k, v=v)
+        return dict(r, k_pre=kh) if c["k_pre"] else r
+    if c["op"] == "pack4":
+        def nearest(x):
+            b = x.double().reshape(-1, 32)
+            amax = b.abs().amax(1, keepdim=True)
+            e = torch.ceil(torch.log2(torch.where(amax > 0, amax, 6.0) / 6))
+            up = torch.exp2(e)
+            grid = torch.tensor(_E2M1, dtype=torch.float64, device=x.device)
+            a = b.abs() / up
+            lo = torch.bucketize(a, grid, right=True) - 1          # grid[lo] <= a
+            hi = (lo + 1).clamp(max=7)
+            dl, dh = a - grid[lo], grid[hi] - a
+            best = torch.where((dh < dl) | ((dh == dl) & (hi % 2 == 0)), hi, lo)
+            return (grid[best] * up * b.sign()).view(x.shape)
+
+        keep = s.live[:, None, :, None]
+        return dict(k=torch.where(keep, nearest(s.req_k), 0.0),
+                    v=torch.where(keep, nearest(s.req_v), 0.0))
+    lens, rows, tables, _ = _layout(c)
+    if 4 * d * hq * sum(len(r) * n for r, n in zip(rows, lens)) > 2e13:
+        return None
+    out = torch.empty(s.T, hq, d, dtype=torch.float64, device="cuda")
+    lse = torch.empty(s.T, hq, dtype=torch.float64, device="cuda")
+    grid = torch.tensor(_E2M1 + [-x for x in _E2M1], dtype=torch.float64, device="cuda")
+
+    def cached(pages, t, which, n):
+        x = pages[torch.tensor(t, device="cuda")]                  # [pages][hkv][page][..]
+        if c["op"] == "attn4":
+            low = x.bitwise_and(15).long()
+            high = x.bitwise_right_shift(4).long()
+            up = torch.pow(2.0, s.scale[torch.tensor(t, device="cuda"), which].double() - 127)
+            x = torch.stack([grid[low], grid[high]], -1).view(*x.shape[:-1], d)
+            x = x * up.repeat_interleave(32, -1)
+        return x.double().permute(1, 0, 2, 3).reshape(hkv, -1, d)[:, :n]
+
+    at = 0
+    for r, n, t in zip(rows, lens, tables):
+        k, v = cached(s.req_k, t, 0, n), cached(s.req_v, t, 1, n)
+        for a in range(0, len(r), 512):
+            ps = torch.tensor(r[a:a + 512], device="cuda")[:, None]
+            j = torch.arange(n, device="cuda")[None]
+            hide = j > ps
+            if c["window"]:
+                hide |= (j <= ps - c["window"]) & (j >= c["sinks"])
+            for h in range(hq):
+                w = s.q[at + a:at + a + 512][:len(ps), h].double() @ k[h // (hq // hkv)].T
+                w = (w / math.sqrt(d)).masked_fill(hide, -math.inf)
+                z = torch.logsumexp(w, 1)
+                lse[at + a:at + a + len(ps), h] = z
+                out[at + a:at + a + len(ps), h] = (w - z[:, None]).exp() @ v[h // (hq // hkv)]
+        at += len(r)
+    return dict(out=out, lse=lse)
