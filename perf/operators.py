@@ -35,8 +35,6 @@ from types import SimpleNamespace
 import torch
 
 own = False
-if own:
-    import paper_2609_32999_amd as P
 
 THETA = 500000.0
 EPS = 1e-6
@@ -249,6 +247,7 @@ def prepare(case, seed):
             if n % page:
                 s.live[t[-1], n % page:] = False
     if own:
+        import paper_2609_32999_amd as P
         kv = "e2m1" if c["op"].endswith("4") else c["kv"]
         m = P.make_model(hq, hkv, d, page, kv, c["kv"], THETA, 65536)
         n = P.tsr_rope_table_bytes(m)
@@ -357,6 +356,7 @@ def _result(s):
 def run(s):
     op, c = s.c["op"], s.c
     if own:
+        import paper_2609_32999_amd as P
         stream = torch.cuda.current_stream()
         if op == "append":
             q, k, v = _heads(s)
