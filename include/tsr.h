@@ -65,7 +65,8 @@ typedef enum {
   TSR_ERR_NO_SPACE = 6       /* not enough free blocks in the cache arena  */
 } tsr_status;
 
-typedef enum { TSR_F32 = 0, TSR_BF16 = 1, TSR_E4M3 = 2 } tsr_dtype;
+/* TSR_E2M1: 4-bit request pages of the steps in tsr_step.h only. */
+typedef enum { TSR_F32 = 0, TSR_BF16 = 1, TSR_E4M3 = 2, TSR_E2M1 = 3 } tsr_dtype;
 
 /* Preparation of a unit (Section 5.1, per-unit plan): a state used from a
  * cache tier is a HIT; a state computed from text is a MISS. */

@@ -1,0 +1,193 @@
+/*
+ * tsr_step.h -- steps over requests whose KV already sits in request pages
+ * (part of the C ABI of libtsr.so; conventions and errors as in tsr.h).
+ *
+ * A composed prefill (tsr.h) leaves every position of a prompt in the
+ * request's pages.  What comes after works on those pages: decoding a token,
+ * extending the prompt by a turn of text, running a layer whose attention has
+ * a sliding window.  A step holds the rows of one such pass:
+ *
+ *   tsr_step_append   per-head norms of queries and keys, RoPE, and the write
+ *                     of the rows' keys and values into their pages;
+ *   tsr_step_attn     attention of the rows over the pages, with a sliding
+ *                     window and sinks if the step was created with them;
+ *   tsr_step_pack_kv, tsr_step_unpack_kv
+ *                     bf16 pages into 4-bit pages and back.
+ *
+ * Page layout as in tsr.h.  A model of kv_dtype TSR_E2M1 (bf16 activations,
+ * head_dim 128, page_size 16, 32 or 64) holds its request pages in 4 bits:
+ *   codes   [n_pages][n_kv_heads][page_size][head_dim / 2] bytes each for K
+ *           and V: dimension 2 i in the low half of byte i, 2 i + 1 in the
+ *           high half; a code is a sign (8) and one of the magnitudes
+ *           0, 0.5, 1, 1.5, 2, 3, 4, 6 (codes 0 .. 7; OCP e2m1);
+ *   scales  [n_pages][2][n_kv_heads][page_size][head_dim / 32] bytes ({K, V}):
+ *           byte b of 32 consecutive dimensions is the factor 2^(b - 127), b
+ *           = 255 NaN (OCP E8M0).
+ * Writing takes the smallest factor 2^k (k >= -126) with max |x| <= 6 * 2^k
+ * (1 for 32 zeros) and rounds x / 2^k to the nearest magnitude, ties to the
+ * even code.  A block that holds a NaN or an infinity gets scale byte 255: it
+ * reads back as NaN.  (Magnitudes from 5 * 2^125 up may read back infinite.)
+ * Such models are for steps only: tsr_plan_create refuses them.
+ *
+ * Step models otherwise: (F32, F32) with head_dim 64, 128 or 256 and
+ * page_size 8 .. 64; (BF16, BF16) with head_dim 128 and page_size 16 .. 64;
+ * any number of query heads per KV head up to 64.  E4M3 pages are refused
+ * (UNSUPPORTED): their one scale a page would have to change, and the page
+ * with it, for every token appended.
+ *
+ * Pointers to K, V, q, out, codes and scales must be 16-byte aligned, lse and
+ * k_pre likewise.  The current device must be the one the buffers are on.
+ */
+#ifndef TSR_STEP_H
+#define TSR_STEP_H
+
+#include <stddef.h>
+#include <stdint.h>
+
+#include "tsr.h"
+
+#ifdef __cplusplus
+extern "C" {
+#endif
+
+/* The rows of one request.
+ *   kv_len       positions 0 .. kv_len-1 of the request have a slot in its
+ *                pages, the rows' own among them; 0 only if it has no row at a position.
+ *   n_rows       rows of this step, >= 0.
+ *   positions    host [n_rows]: the rows' positions, each below kv_len and
+ *                ascending; -1 marks a row that holds no token (a batch padded
+ *                to a fixed size): nothing is appended for it and its output
+ *                is 0 with lse -inf.  NULL: the last n_rows positions.
+ *   row_lo       host [n_rows]: first visible key of each row, 0 ..
+ *                position + 1 (position + 1: it sees nothing, output 0, lse
+ *                -inf); any value for a -1 row.  NULL: 0.  tsr_plan_row_kv_lo
+ *                of a composed prompt's rows goes here.
+ *   block_table  host [ceil(kv_len / page_size)] request page ids.  Requests
+ *                may share pages they only read (a common prefix); a page
+ *                that a row is appended to belongs to one request alone (else
+ *                tsr_step_append refuses the step). */
+typedef struct {
+  int32_t kv_len;
+  int32_t n_rows;
+  const int32_t* positions;
+  const int32_t* row_lo;
+  const int32_t* block_table;
+} tsr_step_request;
+
+/* Options (NULL: all zero).
+ *   window, n_sinks  a row at position p with first key lo sees the keys
+ *                j in [lo, p] with  j > p - window  or  j < lo + n_sinks:
+ *                the last `window` positions, itself among them, and the
+ *                first n_sinks keys, which stay visible.  window 0: every
+ *                key in [lo, p].
+ *   split_tiles  > 0: key ranges longer than that many 32-key tiles are cut
+ *                into equal ranges run side by side and merged by a second
+ *                kernel; 0: cut where the launch would leave compute units
+ *                idle; -1: never.  A step with cut ranges writes a buffer in
+ *                its workspace on every tsr_step_attn call: calls that use
+ *                one step on streams that run concurrently race there.
+ *   attn_kernel  0: by the rule of tsr_step_attn; 1: the kernel for few rows;
+ *                2: the one for many (bf16 activations only).
+ *   reserved     must be zero. */
+typedef struct {
+  int32_t window;
+  int32_t n_sinks;
+  int32_t split_tiles;
+  int32_t attn_kernel;
+  int32_t reserved[4];
+} tsr_step_options;
+
+/* RMS norms of each query and key head:
+ *   n(x) = x / sqrt(mean_i x_i^2 + eps) * w      (fp32)
+ *   q_weight, k_weight  device [head_dim] of act dtype, 16-byte aligned;
+ *                       NULL: ones.
+ *   eps                 > 0, finite. */
+typedef struct {
+  const void* q_weight;
+  const void* k_weight;
+  float eps;
+  int32_t reserved;   /* must be zero */
+} tsr_qk_norm;
+
+typedef struct tsr_step tsr_step;
+
+/* Device workspace bytes of tsr_step_create for this batch, or 0 if it fails
+ * validation (tsr_last_error says why). */
+size_t tsr_step_workspace_size(const tsr_model* model, const tsr_step_request* reqs,
+                               int32_t n_req, int32_t n_req_pages,
+                               const tsr_step_options* options);
+
+/* Validate a batch and build its step.  The device image is copied into
+ * dev_workspace (256-byte aligned) with hipMemcpyAsync on `stream`;
+ * dev_workspace NULL builds a step that can be inspected but not executed (no
+ * HIP call is made).  dev_rope_table: a table of tsr_rope_table_init for the
+ * model.  Rows are in the order given: requests in order, and within a
+ * request its rows in order.  A step is immutable and serves every layer of
+ * the model. */
+tsr_status tsr_step_create(const tsr_model* model, const tsr_step_request* reqs, int32_t n_req,
+                           int32_t n_req_pages, const tsr_step_options* options,
+                           const void* dev_rope_table, void* dev_workspace,
+                           size_t workspace_bytes, void* stream, tsr_step** out_step);
+void tsr_step_destroy(tsr_step* step);
+
+/* Rows T; attention work items; items whose key range was cut; rows an item
+ * of the attention kernel holds, times query heads (16 or 128).  -1 for NULL. */
+int32_t tsr_step_num_rows(const tsr_step* step);
+int32_t tsr_step_num_attn_items(const tsr_step* step);
+int32_t tsr_step_num_attn_splits(const tsr_step* step);
+int32_t tsr_step_attn_item_rows(const tsr_step* step);
+
+/* For every row t at position p_t >= 0, in one pass:
+ *   q_out[t] = RoPE(n_q(q[t]), p_t)
+ *   k^[t]    = n_k(k[t]) rounded to the activation type, the form a unit
+ *              cache keeps; also written to k_pre[t] if that is not NULL
+ *              (tsr_retain_kv takes it as its k)
+ *   K[p_t]   = RoPE(k^[t], p_t),  V[p_t] = v[t]     into the request pages
+ * n_q, n_k as in tsr_qk_norm (norm NULL: the identity).  K is rotated from
+ * its rounded form so that a unit composed from the cache (tsr_compose_kv)
+ * holds the very bits written here.  Rotation as in tsr_compose_kv; results
+ * are rounded once.  4-bit pages: K and V are written as codes and scales.
+ *   q, k, v   device [T][heads][head_dim] of act dtype; rows q_stride,
+ *             k_stride, v_stride elements apart (0: packed), multiples of 16
+ *             bytes, so that one projection's output serves all three.
+ *   q_out     device [T][n_q_heads][head_dim]; may be q itself if packed.
+ *   k_pre     device [T][n_kv_heads][head_dim] or NULL; may be k if packed.
+ *   req_scale 4-bit pages only, else NULL.
+ * Rows of -1 leave everything as it was, their rows of q_out and k_pre too. */
+tsr_status tsr_step_append(const tsr_step* step, const tsr_qk_norm* norm, const void* q,
+                           int64_t q_stride, const void* k, int64_t k_stride, const void* v,
+                           int64_t v_stride, void* q_out, void* k_pre, void* req_k, void* req_v,
+                           void* req_scale, void* stream);
+
+/* o_t,h = softmax(scale * q_t,h . K_j,g) V_j,g over the visible keys j, g =
+ * h / (n_q_heads / n_kv_heads), lse its natural log-sum-exp.
+ *   q     device [T][n_q_heads][head_dim], rotated (tsr_step_append's q_out).
+ *   out   device [T][n_q_heads][head_dim] of act dtype.
+ *   lse   device [T][n_q_heads] fp32, or NULL.
+ * Every position that a row sees must have been written.  Keys that a row
+ * does not see do not reach its output, whatever they hold.  Scores and sums
+ * are fp32 (fp64 for fp32 models).
+ * Two kernels for bf16 activations.  For few rows (16 rows x heads an item,
+ * bound by reading the pages) the probabilities enter the second product as
+ * two bf16 parts.  For many (128 an item, bound by the matrix cores) they and
+ * the values enter it as fp16: a value beyond 65504 in magnitude makes the
+ * outputs that see it non-finite.  The second serves steps whose requests
+ * have rows enough to fill its items. */
+tsr_status tsr_step_attn(const tsr_step* step, const void* q, const void* req_k,
+                         const void* req_v, const void* req_scale, void* out, float* lse,
+                         void* stream);
+
+/* bf16 request pages -> 4-bit request pages and back, positions 0 ..
+ * kv_len - 1 of the step's requests, page for page under the same ids (steps
+ * of a TSR_E2M1 model).  Other slots are left as they were.
+ *   bf16_k, bf16_v  device [n_req_pages][n_kv_heads][page_size][head_dim]. */
+tsr_status tsr_step_pack_kv(const tsr_step* step, const void* bf16_k, const void* bf16_v,
+                            void* req_k, void* req_v, void* req_scale, void* stream);
+tsr_status tsr_step_unpack_kv(const tsr_step* step, const void* req_k, const void* req_v,
+                              const void* req_scale, void* bf16_k, void* bf16_v, void* stream);
+
+#ifdef __cplusplus
+}
+#endif
+
+#endif /* TSR_STEP_H */

@@ -14,7 +14,10 @@ from ._binding import (DTYPE_CODES, EXPORTS, TSR_ATTN_AFTER_COMPOSE, TSR_ATTN_AL
                        tsr_abi_version, tsr_append_kv, tsr_assemble_kv, tsr_attn, tsr_attn_part, tsr_compose_kv, tsr_last_error,
                        tsr_peak_copy, tsr_peak_mfma, tsr_peak_mfma_flops,
                        tsr_plan_create, tsr_plan_workspace_size, tsr_prefill_attn,
-                       tsr_retain_kv, tsr_rope_table_bytes, tsr_rope_table_init)
+                       tsr_retain_kv, tsr_rope_table_bytes, tsr_rope_table_init,
+                       TSR_E2M1, Step, StepBatch, make_qk_norm, tsr_step_append,
+                       tsr_step_attn, tsr_step_create, tsr_step_pack_kv, tsr_step_unpack_kv,
+                       tsr_step_workspace_size)
 
 __all__ = [
     "DTYPE_CODES", "EXPORTS", "TSR_ATTN_AFTER_COMPOSE", "TSR_ATTN_ALL", "TSR_ATTN_BEFORE_COMPOSE", "TSR_E4M3", "TSR_BF16", "TSR_ENTRY_ABSENT",
@@ -26,4 +29,6 @@ __all__ = [
     "tsr_last_error", "tsr_peak_copy", "tsr_peak_mfma", "tsr_peak_mfma_flops",
     "tsr_plan_create", "tsr_plan_workspace_size", "tsr_prefill_attn",
     "tsr_retain_kv", "tsr_rope_table_bytes", "tsr_rope_table_init",
+    "TSR_E2M1", "Step", "StepBatch", "make_qk_norm", "tsr_step_append", "tsr_step_attn",
+    "tsr_step_create", "tsr_step_pack_kv", "tsr_step_unpack_kv", "tsr_step_workspace_size",
 ]

@@ -23,8 +23,8 @@ LIB_PATH = os.environ.get("TSR_LIBRARY") or os.path.join(HERE, "libtsr.so")
 STATUS_NAMES = {0: "OK", 1: "INVALID_ARG", 2: "UNSUPPORTED", 3: "OUT_OF_RANGE", 4: "DEVICE",
                 5: "STATE", 6: "NO_SPACE"}
 TSR_ENTRY_ABSENT, TSR_ENTRY_PENDING, TSR_ENTRY_READY = 0, 1, 2
-TSR_F32, TSR_BF16, TSR_E4M3 = 0, 1, 2
-DTYPE_CODES = {"f32": TSR_F32, "bf16": TSR_BF16, "e4m3": TSR_E4M3}
+TSR_F32, TSR_BF16, TSR_E4M3, TSR_E2M1 = 0, 1, 2, 3
+DTYPE_CODES = {"f32": TSR_F32, "bf16": TSR_BF16, "e4m3": TSR_E4M3, "e2m1": TSR_E2M1}
 TSR_MISS, TSR_HIT = 0, 1
 TSR_SCOPE_GLOBAL, TSR_SCOPE_LOCAL = 0, 1
 TSR_ATTN_ALL, TSR_ATTN_BEFORE_COMPOSE, TSR_ATTN_AFTER_COMPOSE = 0, 1, 2
@@ -49,6 +49,10 @@ EXPORTS = (
     "tsr_scorer_counts", "tsr_window_for_capacity", "tsr_admitter_create",
     "tsr_admitter_destroy", "tsr_admit", "tsr_admitter_remove", "tsr_admitter_blocks",
     "tsr_admitter_used_blocks", "tsr_admitter_num_units", "tsr_route", "tsr_replay",
+    # include/tsr_step.h
+    "tsr_step_workspace_size", "tsr_step_create", "tsr_step_destroy", "tsr_step_num_rows",
+    "tsr_step_num_attn_items", "tsr_step_num_attn_splits", "tsr_step_attn_item_rows",
+    "tsr_step_append", "tsr_step_attn", "tsr_step_pack_kv", "tsr_step_unpack_kv",
 )
 
 
@@ -84,6 +88,21 @@ class tsr_request(ctypes.Structure):
 class tsr_plan_options(ctypes.Structure):
     _fields_ = [("alias_v", c_int32), ("alias_k", c_int32), ("split_tiles", c_int32),
                 ("attn_kernel", c_int32), ("reserved", c_int32 * 4)]
+
+
+class tsr_step_request(ctypes.Structure):
+    _fields_ = [("kv_len", c_int32), ("n_rows", c_int32), ("positions", POINTER(c_int32)),
+                ("row_lo", POINTER(c_int32)), ("block_table", POINTER(c_int32))]
+
+
+class tsr_step_options(ctypes.Structure):
+    _fields_ = [("window", c_int32), ("n_sinks", c_int32), ("split_tiles", c_int32),
+                ("attn_kernel", c_int32), ("reserved", c_int32 * 4)]
+
+
+class tsr_qk_norm(ctypes.Structure):
+    _fields_ = [("q_weight", c_void_p), ("k_weight", c_void_p), ("eps", c_float),
+                ("reserved", c_int32)]
 
 
 class tsr_replay_config(ctypes.Structure):
@@ -195,6 +214,21 @@ def lib():
             "tsr_replay": (c_int32, [POINTER(tsr_replay_config), POINTER(c_int32),
                                      POINTER(c_uint64), POINTER(c_int32), c_int32,
                                      POINTER(tsr_replay_stats), POINTER(c_int32)]),
+            "tsr_step_workspace_size": (c_size_t, [POINTER(tsr_model), POINTER(tsr_step_request),
+                                                   c_int32, c_int32, POINTER(tsr_step_options)]),
+            "tsr_step_create": (c_int32, [POINTER(tsr_model), POINTER(tsr_step_request), c_int32,
+                                          c_int32, POINTER(tsr_step_options), P, P, c_size_t, P,
+                                          POINTER(c_void_p)]),
+            "tsr_step_destroy": (None, [P]),
+            "tsr_step_num_rows": (c_int32, [P]),
+            "tsr_step_num_attn_items": (c_int32, [P]),
+            "tsr_step_num_attn_splits": (c_int32, [P]),
+            "tsr_step_attn_item_rows": (c_int32, [P]),
+            "tsr_step_append": (c_int32, [P, POINTER(tsr_qk_norm), P, c_int64, P, c_int64, P,
+                                          c_int64, P, P, P, P, P, P]),
+            "tsr_step_attn": (c_int32, [P, P, P, P, P, P, P, P]),
+            "tsr_step_pack_kv": (c_int32, [P, P, P, P, P, P, P]),
+            "tsr_step_unpack_kv": (c_int32, [P, P, P, P, P, P, P]),
         }
         for name, (res, args) in sig.items():
             f = getattr(L, name)
@@ -663,3 +697,123 @@ def tsr_attn_aliased(plan: Plan, part: int, q, req_k, req_v, pool_k, pool_v, out
     _check(lib().tsr_attn_aliased(plan.handle, part, _ptr(q), _ptr(req_k), _ptr(req_v),
                                   _ptr(pool_k), _ptr(pool_v), _ptr(out), _ptr(lse),
                                   _stream(stream)))
+
+
+# ------------------------------------------------- steps over request pages
+class StepBatch:
+    """ctypes arrays for the requests of a step.
+
+    Each request needs `kv_len`, `n_rows` and `block_table`, and may carry
+    `positions` and `row_lo` (sequences of n_rows, or None).  The arrays stay
+    alive as long as this object.
+    """
+
+    def __init__(self, requests):
+        self._keep = []
+        self.array = (tsr_step_request * max(1, len(requests)))()
+        self.n = len(requests)
+        for i, r in enumerate(requests):
+            ptrs = []
+            for name in ("positions", "row_lo", "block_table"):
+                a = getattr(r, name, None)
+                if a is None:
+                    ptrs.append(None)
+                    continue
+                a = _i32(a)
+                if name != "block_table" and a.shape != (int(r.n_rows),):
+                    raise ValueError(f"request {i}: {name} does not hold n_rows entries")
+                self._keep.append(a)
+                ptrs.append(_i32p(a))
+            self.array[i] = tsr_step_request(int(r.kv_len), int(r.n_rows), *ptrs)
+
+
+def _step_options(window: int, n_sinks: int, split_tiles: int, attn_kernel: int):
+    return tsr_step_options(window=window, n_sinks=n_sinks, split_tiles=split_tiles,
+                            attn_kernel=attn_kernel)
+
+
+def tsr_step_workspace_size(model: tsr_model, batch: StepBatch, n_req_pages: int,
+                            window: int = 0, n_sinks: int = 0, split_tiles: int = 0,
+                            attn_kernel: int = 0) -> int:
+    opts = _step_options(window, n_sinks, split_tiles, attn_kernel)
+    n = lib().tsr_step_workspace_size(ctypes.byref(model), batch.array, batch.n, n_req_pages,
+                                      ctypes.byref(opts))
+    if n == 0:
+        raise TsrError(TSR_ERR_INVALID_ARG, tsr_last_error())
+    return n
+
+
+class Step:
+    """Owner of a tsr_step handle."""
+
+    def __init__(self, handle: int, model: tsr_model):
+        self.handle = handle
+        self.model = model
+
+    @property
+    def num_rows(self) -> int:
+        return lib().tsr_step_num_rows(self.handle)
+
+    @property
+    def num_attn_items(self) -> int:
+        return lib().tsr_step_num_attn_items(self.handle)
+
+    @property
+    def num_attn_splits(self) -> int:
+        return lib().tsr_step_num_attn_splits(self.handle)
+
+    @property
+    def attn_item_rows(self) -> int:
+        return lib().tsr_step_attn_item_rows(self.handle)
+
+    def destroy(self) -> None:
+        if self.handle:
+            lib().tsr_step_destroy(self.handle)
+            self.handle = None
+
+    def __del__(self):
+        try:
+            self.destroy()
+        except Exception:
+            pass
+
+
+def tsr_step_create(model: tsr_model, batch: StepBatch, n_req_pages: int, dev_rope_table=None,
+                    dev_workspace=None, workspace_bytes: int = 0, stream=None, window: int = 0,
+                    n_sinks: int = 0, split_tiles: int = 0, attn_kernel: int = 0) -> Step:
+    out = c_void_p()
+    opts = _step_options(window, n_sinks, split_tiles, attn_kernel)
+    _check(lib().tsr_step_create(ctypes.byref(model), batch.array, batch.n, n_req_pages,
+                                 ctypes.byref(opts), _ptr(dev_rope_table), _ptr(dev_workspace),
+                                 workspace_bytes, _stream(stream), ctypes.byref(out)))
+    return Step(out.value, model)
+
+
+def make_qk_norm(q_weight=None, k_weight=None, eps: float = 1e-6) -> tsr_qk_norm:
+    """Weights of the query and key norms (device [head_dim] of the activation
+    type, or None for ones); the caller keeps them alive."""
+    return tsr_qk_norm(q_weight=_ptr(q_weight), k_weight=_ptr(k_weight), eps=float(eps))
+
+
+def tsr_step_append(step: Step, q, k, v, req_k, req_v, req_scale, q_out, k_pre=None, norm=None,
+                    q_stride: int = 0, k_stride: int = 0, v_stride: int = 0,
+                    stream=None) -> None:
+    _check(lib().tsr_step_append(step.handle, ctypes.byref(norm) if norm is not None else None,
+                                 _ptr(q), q_stride, _ptr(k), k_stride, _ptr(v), v_stride,
+                                 _ptr(q_out), _ptr(k_pre), _ptr(req_k), _ptr(req_v),
+                                 _ptr(req_scale), _stream(stream)))
+
+
+def tsr_step_attn(step: Step, q, req_k, req_v, req_scale, out, lse=None, stream=None) -> None:
+    _check(lib().tsr_step_attn(step.handle, _ptr(q), _ptr(req_k), _ptr(req_v), _ptr(req_scale),
+                               _ptr(out), _ptr(lse), _stream(stream)))
+
+
+def tsr_step_pack_kv(step: Step, bf16_k, bf16_v, req_k, req_v, req_scale, stream=None) -> None:
+    _check(lib().tsr_step_pack_kv(step.handle, _ptr(bf16_k), _ptr(bf16_v), _ptr(req_k),
+                                  _ptr(req_v), _ptr(req_scale), _stream(stream)))
+
+
+def tsr_step_unpack_kv(step: Step, req_k, req_v, req_scale, bf16_k, bf16_v, stream=None) -> None:
+    _check(lib().tsr_step_unpack_kv(step.handle, _ptr(req_k), _ptr(req_v), _ptr(req_scale),
+                                    _ptr(bf16_k), _ptr(bf16_v), _stream(stream)))

@@ -8,6 +8,7 @@
 #include <string>
 #include <vector>
 
+#include "step_internal.h"
 #include "tsr_internal.h"
 
 namespace tsr {
@@ -25,6 +26,11 @@ tsr_status check_exec(const tsr_plan* p) {
     return TSR_ERR_INVALID_ARG;
   }
   return check_static_plan(p);
+}
+
+// The table serves plans and steps: a model that either takes.
+tsr_status check_rope_model(const tsr_model* m) {
+  return check_step_model(m) == TSR_OK ? TSR_OK : check_model(m);
 }
 
 bool is_e4m3(const tsr_plan* p) { return p->model.kv_dtype == TSR_E4M3; }
@@ -226,14 +232,14 @@ int32_t tsr_abi_version(void) { return TSR_ABI_VERSION; }
 const char* tsr_last_error(void) { return g_error.c_str(); }
 
 size_t tsr_rope_table_bytes(const tsr_model* model) {
-  if (check_model(model) != TSR_OK) return 0;
+  if (check_rope_model(model) != TSR_OK) return 0;
   return 2 * (size_t)model->max_position * (size_t)(model->head_dim / 2) * sizeof(float);
 }
 
 tsr_status tsr_rope_table_init(const tsr_model* model, void* dev_table,
                                size_t table_bytes, void* stream) {
   return guarded([&]() -> tsr_status {
-    tsr_status st = check_model(model);
+    tsr_status st = check_rope_model(model);
     if (st != TSR_OK) return st;
     const size_t need = tsr_rope_table_bytes(model);
     if (!dev_table || table_bytes < need) {

@@ -1,0 +1,52 @@
+// 4-bit pages (tsr_step.h): e2m1 codes, one E8M0 scale byte per 32 dims.
+// gfx950 converts between pairs of codes and fp32 or bf16 under a power-of-two
+// scale in one instruction, rounding to nearest even; of the scale operand
+// only the exponent counts, and exponent 255 (scale byte 255) reads as NaN.
+#pragma once
+
+#include <hip/hip_runtime.h>
+
+#include <cstdint>
+
+namespace tsr {
+
+constexpr int kScaleDims = 32;
+
+// Scale byte of a block whose largest magnitude is amax: the smallest k >= -126
+// with amax <= 6 * 2^k, plus 127; 127 for zeros, 255 if `finite` is false.
+__device__ __forceinline__ uint32_t e2m1_scale(float amax, bool finite) {
+  if (!finite) return 255;
+  if (amax == 0.0f) return 127;
+  // amax = f * 2^e, f in [1, 2): 6 = 1.5 * 2^2.  (fp32 subnormals, e = -127
+  // here, end at the least scale like the smallest normal numbers.)
+  const uint32_t u = __float_as_uint(amax);
+  const int e = (int)(u >> 23) - 127;
+  const int k = (u & 0x7fffffu) <= 0x400000u ? e - 2 : e - 1;
+  return (uint32_t)(max(k, -126) + 127);
+}
+
+__device__ __forceinline__ float e2m1_factor(uint32_t scale_byte) {
+  return __uint_as_float(scale_byte << 23);
+}
+
+// Eight values -> eight codes (x[0] in the low half of byte 0).
+__device__ __forceinline__ uint32_t e2m1_encode8(const float* x, float factor) {
+  uint32_t c = 0;
+  c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, x[0], x[1], factor, 0);
+  c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, x[2], x[3], factor, 1);
+  c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, x[4], x[5], factor, 2);
+  c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, x[6], x[7], factor, 3);
+  return c;
+}
+
+// Eight codes -> eight bf16 values (exact).
+__device__ __forceinline__ uint4 e2m1_decode8(uint32_t c, float factor) {
+  uint4 r;
+  r.x = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, factor, 0));
+  r.y = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, factor, 1));
+  r.z = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, factor, 2));
+  r.w = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, factor, 3));
+  return r;
+}
+
+}  // namespace tsr

@@ -20,6 +20,7 @@
 #include <numeric>
 #include <sstream>
 
+#include "step_internal.h"
 #include "tsr_internal.h"
 
 namespace tsr {
@@ -42,7 +43,7 @@ struct Seg {
 
 }  // namespace
 
-tsr_status check_model(const tsr_model* m) {
+tsr_status check_model_fields(const tsr_model* m) {
   if (!m) return fail(TSR_ERR_INVALID_ARG, "model is NULL");
   if (m->n_q_heads <= 0 || m->n_kv_heads <= 0)
     return fail(TSR_ERR_INVALID_ARG, "head counts must be positive");
@@ -62,6 +63,12 @@ tsr_status check_model(const tsr_model* m) {
     return fail(TSR_ERR_INVALID_ARG, "max_position must be in [1, 2^20]");
   if (!(m->softmax_scale >= 0.0f) || !std::isfinite(m->softmax_scale))
     return fail(TSR_ERR_INVALID_ARG, "softmax_scale must be >= 0 and finite");
+  return TSR_OK;
+}
+
+tsr_status check_model(const tsr_model* m) {
+  tsr_status st = check_model_fields(m);
+  if (st != TSR_OK) return st;
   const int G = m->n_q_heads / m->n_kv_heads;
   if (m->kv_dtype == TSR_F32 && m->act_dtype == TSR_F32) {
     if (m->head_dim != 64 && m->head_dim != 128 && m->head_dim != 256)

@@ -1,0 +1,730 @@
+// Attention of a step's rows over request pages (tsr_step.h), for few rows
+// per request: decoding, short extensions, any step of an fp32 model.
+//
+//   o = softmax(scale * q . K^T) V   over the keys a row sees:
+//   lo <= j <= pos  and  (j > pos - window  or  j < lo + n_sinks)
+//
+// Rows of one request times the query heads of one KV head, 16 vectors, are
+// one operand of a 16 x 16 matrix instruction; the launch is bound by reading
+// the pages, so each K and V byte is asked for once per item, far ahead.
+//
+//   step_attn_kernel   bf16 and 4-bit pages
+//   step_attn_f32_kernel
+//   step_merge_kernel  joins the key ranges of cut items
+#include <cmath>
+
+#include "attn_common.h"
+#include "e2m1.h"
+#include "kernels_common.h"
+#include "step_internal.h"
+
+namespace tsr {
+
+namespace {
+
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+
+struct StepAttnArgs {
+  const StepRow* rows;
+  const StepItem* items;
+  const int32_t* bts;
+  const void *q, *k, *v;
+  const uint8_t* scales;
+  void* out;
+  float *lse, *split_o, *split_lse;
+  int32_t n_q_heads, n_kv_heads, log2_page, window, n_sinks;
+  float scale, scale_log2e;
+};
+
+// Keys a row sees: [wlo, pos] and [lo, shi); nothing if pos < 0.
+struct Sight {
+  int32_t lo, shi, wlo, pos;
+};
+__device__ __forceinline__ Sight row_sight(const StepRow& r, int window, int n_sinks) {
+  Sight s{r.lo, r.lo + n_sinks, r.lo, r.pos};
+  if (window > 0) s.wlo = max(r.lo, r.pos - window + 1);
+  return s;
+}
+__device__ __forceinline__ bool sees(const Sight& s, int key) {
+  return (key <= s.pos) & (key >= s.lo) & ((key >= s.wlo) | (key < s.shi));
+}
+
+// A uniform 32-bit load through the scalar cache.
+__device__ __forceinline__ int32_t uniform_i32(const int32_t* p) {
+  return *reinterpret_cast<const __attribute__((address_space(4))) int32_t*>(
+      reinterpret_cast<uintptr_t>(p));
+}
+
+template <int N>
+__device__ __forceinline__ void wait_vm() {
+  asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
+}
+__device__ __forceinline__ void wait_lds() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
+
+// Direct global->LDS loads, lane l's bytes at lds + 16 l (or 4 l): base
+// uniform, `off` the lane's byte offset.  The memory clobber keeps LDS reads
+// of the buffer on their side of it.
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"
+__device__ __forceinline__ void dma16(const void* base, uint32_t off, uint32_t lds) {
+  asm volatile("s_mov_b32 m0, %2\n\tglobal_load_lds_dwordx4 %0, %1"
+               :: "v"(off), "s"(base), "s"(lds) : "m0", "memory");
+}
+__device__ __forceinline__ void dma4(const void* base, uint32_t off, uint32_t lds) {
+  asm volatile("s_mov_b32 m0, %2\n\tglobal_load_lds_dword %0, %1"
+               :: "v"(off), "s"(base), "s"(lds) : "m0", "memory");
+}
+#pragma clang diagnostic pop
+
+// ------------------------------------------------ bf16 and 4-bit pages
+// A wave takes every fourth 32-key tile of the item's range and works alone
+// until the four join at the end: its tiles arrive in LDS by direct loads,
+// kStages of them under way, and nothing but its own counter is waited for.
+//   S^T = K Q^T     16x16x32, two 16-key blocks: lane l holds query vector
+//                   l % 16 and keys 4 (l / 16) + 0 .. 3 of each block
+//   O^T += V^T P^T  16x16x32: those eight keys are the lane's operand, so P
+//                   stays in its registers; V^T comes from V's rows in LDS by
+//                   transposing reads (four keys x 16 dims a read)
+// P enters as two bf16 parts (hi + the rest), which keeps it exact to 2^-17:
+// with hi alone the output's error would be 1.4 times that of its rounding.
+// The products are far from the bound, so the second one costs nothing.
+//
+// bf16: a K block lies as four 1 KB runs of 32 dims, [chunk of 8 dims][key],
+// the order of the operand; a V row's 16-byte chunks are permuted by its key
+// (kVSwz) so that a transposing read touches every bank once.
+// 4-bit: codes arrive like K's operand, [32-dim block][key]; V's become bf16
+// rows in a buffer of the wave's own first.
+template <bool F4> struct Tile;
+template <> struct Tile<false> {
+  static constexpr int kStages = 2, kBytes = 16384, kLoads = 16, kRows = 0;
+};
+template <> struct Tile<true> {
+  static constexpr int kStages = 4, kBytes = 4608, kLoads = 6, kRows = 8192;
+};
+constexpr int kStepWaves = 4;
+
+template <bool F4>
+__global__ __launch_bounds__(64 * kStepWaves) void step_attn_kernel(const StepAttnArgs a) {
+  using T = Tile<F4>;
+  constexpr int NW = kStepWaves, ST = T::kStages;
+  constexpr int kWaveLds = ST * T::kBytes + T::kRows;
+  constexpr int kOStr = kD + 4;   // floats per vector while the waves join
+  static_assert(NW * kStepVecs * (kOStr + 2) * 4 <= NW * kWaveLds, "the join fits the tiles");
+  __shared__ __attribute__((aligned(1024))) uint8_t lds[NW * kWaveLds];
+
+  const StepItem it = a.items[blockIdx.x];
+  if (it.n_rows == 0) return;
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int c16 = lane & 15, c4 = lane >> 4;
+  const int G = a.n_q_heads / a.n_kv_heads;
+  const int page_mask = (1 << a.log2_page) - 1;
+  const int32_t* bt = a.bts + it.bt_off;
+
+  // ---- tiles of this wave
+  uint8_t* mine = lds + w * kWaveLds;
+  const uint32_t mine_at = lds_addr(mine);
+  const int na = it.a1 - it.a0, nt = na + it.b1 - it.b0;
+  const int n = nt > w ? (nt - w + NW - 1) / NW : 0;
+  auto tile_key = [&](int i) {
+    const int t = w + NW * i;
+    return kStepKeys * (t < na ? it.a0 + t : it.b0 + t - na);
+  };
+  // a 16-key block past the last key stands in for nothing: the last block is
+  // read again (every score of it is masked), and within it the last key
+  const int last = it.kv_len - 1, last_blk = last & ~15;
+  auto page_of = [&](int key) { return uniform_i32(bt + (min(key, last_blk) >> a.log2_page)); };
+  // V rows: key k keeps 16-byte chunk c at place c ^ 2 (k % 8)
+  const int vkey = lane >> 4, vpos = lane & 15;
+  int pg[2] = {0, 0};
+  auto fetch_pages = [&](int i) {
+    const int key0 = tile_key(i);
+    pg[0] = page_of(key0);
+    pg[1] = page_of(key0 + 16);
+  };
+  auto issue = [&](int i, int stage) __attribute__((always_inline)) {
+    const int key0 = tile_key(i);
+    const uint32_t dst = mine_at + stage * T::kBytes;
+#pragma unroll
+    for (int b = 0; b < 2; ++b) {
+      const int kb = min(key0 + 16 * b, last_blk);
+      const int top = last - kb;               // last key of the block to read
+      const int64_t slot = ((((int64_t)pg[b] * a.n_kv_heads + it.kv_head) << a.log2_page) +
+                            (kb & page_mask));
+      const int kk = min(c16, top);
+      if constexpr (!F4) {
+        const uint8_t* kp = static_cast<const uint8_t*>(a.k) + slot * (2 * kD);
+        const uint8_t* vp = static_cast<const uint8_t*>(a.v) + slot * (2 * kD);
+#pragma unroll
+        for (int s = 0; s < 4; ++s)
+          dma16(kp, kk * (2 * kD) + 64 * s + 16 * c4, dst + 4096 * b + 1024 * s);
+#pragma unroll
+        for (int s = 0; s < 4; ++s) {
+          const int k = 4 * s + vkey;
+          dma16(vp, min(k, top) * (2 * kD) + 16 * (vpos ^ (2 * (k & 7))),
+                dst + 8192 + 4096 * b + 1024 * s);
+        }
+      } else {
+        const uint8_t* kp = static_cast<const uint8_t*>(a.k) + slot * (kD / 2);
+        const uint8_t* vp = static_cast<const uint8_t*>(a.v) + slot * (kD / 2);
+        dma16(kp, kk * (kD / 2) + 16 * c4, dst + 1024 * b);
+        dma16(vp, kk * (kD / 2) + 16 * c4, dst + 2048 + 1024 * b);
+        // lanes 0 .. 15 the keys' K scales, 16 .. 31 their V scales
+        const int64_t ks = ((((int64_t)pg[b] * 2 * a.n_kv_heads + it.kv_head) << a.log2_page) +
+                            (kb & page_mask));
+        const uint32_t vs = ((uint32_t)a.n_kv_heads << a.log2_page) * (c4 & 1);
+        dma4(a.scales + ks * (kD / kScaleDims), (kk + vs) * (kD / kScaleDims),
+             dst + 4096 + 256 * b);
+      }
+    }
+  };
+
+  // the first tiles are on their way while the queries come
+#pragma unroll
+  for (int i = 0; i < ST - 1; ++i)
+    if (i < n) {
+      fetch_pages(i);
+      issue(i, i);
+    }
+  if (ST - 1 < n) fetch_pages(ST - 1);
+  // this lane's query vector (past the item's last: its first row again)
+  int vr = c16 / it.n_heads, vh = c16 - vr * it.n_heads;
+  if (vr >= it.n_rows) vr = vh = 0;
+  const Sight sight = row_sight(a.rows[it.row0 + vr], a.window, a.n_sinks);
+  Frag qf[4];
+  {
+    const uint16_t* qp = static_cast<const uint16_t*>(a.q) +
+                         ((int64_t)(it.row0 + vr) * a.n_q_heads + it.kv_head * G + it.head0 + vh) *
+                             kD;
+#pragma unroll
+    for (int s = 0; s < 4; ++s)
+      qf[s].u = *reinterpret_cast<const uint4*>(qp + (F4 ? 32 * c4 + 8 * s : 32 * s + 8 * c4));
+  }
+
+  // The queries are here before the loop: a wait for them inside it would be
+  // one for the loads that it keeps under way.
+#pragma unroll
+  for (int s = 0; s < 4; ++s)
+    asm volatile("" : "+v"(qf[s].w[0]), "+v"(qf[s].w[1]), "+v"(qf[s].w[2]), "+v"(qf[s].w[3]));
+
+  f32x4 o[8];
+#pragma unroll
+  for (int db = 0; db < 8; ++db) o[db] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+  float m = -INFINITY, l = 0.0f;
+  const float sc = a.scale_log2e;
+  // transposing reads: lane l of a group of 16 points at key l / 4 (of four),
+  // 8 bytes l % 4 of the 16 dims
+  const int tkey = 4 * c4 + (c16 >> 2);
+  const uint32_t toff = tkey * (2 * kD) + 32 * (tkey & 7) + 8 * (c16 & 3);
+
+  auto tile = [&](int key0, const uint8_t* t) __attribute__((always_inline)) {
+    // ---- scores
+    f32x4 s[2];
+    uint8_t* vrows;
+    if constexpr (!F4) {
+      vrows = const_cast<uint8_t*>(t) + 8192;
+#pragma unroll
+      for (int b = 0; b < 2; ++b) {
+        s[b] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          Frag f;
+          f.u = *reinterpret_cast<const uint4*>(t + 4096 * b + 1024 * k + 16 * lane);
+          s[b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f.b, qf[k].b, s[b], 0, 0, 0);
+        }
+      }
+    } else {
+      vrows = mine + ST * T::kBytes;
+#pragma unroll
+      for (int b = 0; b < 2; ++b) {
+        const uint4 kc = *reinterpret_cast<const uint4*>(t + 1024 * b + 16 * lane);
+        const uint4 vc = *reinterpret_cast<const uint4*>(t + 2048 + 1024 * b + 16 * lane);
+        const uint8_t* sp = t + 4096 + 256 * b + 4 * c16 + c4;
+        const float kf = e2m1_factor(sp[0]), vf = e2m1_factor(sp[64]);
+        const uint32_t kw[4] = {kc.x, kc.y, kc.z, kc.w}, vw[4] = {vc.x, vc.y, vc.z, vc.w};
+        s[b] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          Frag f;
+          f.u = e2m1_decode8(kw[k], kf);
+          s[b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f.b, qf[k].b, s[b], 0, 0, 0);
+        }
+        // V to bf16 rows: the lane's key and 32 dims
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+          *reinterpret_cast<uint4*>(vrows + (16 * b + c16) * (2 * kD) +
+                                    16 * ((4 * c4 + k) ^ (2 * (c16 & 7)))) =
+              e2m1_decode8(vw[k], vf);
+      }
+    }
+    const bool masked = key0 < it.full_lo || key0 + kStepKeys - 1 > it.full_hi;
+    if (masked) {
+#pragma unroll
+      for (int b = 0; b < 2; ++b)
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+          if (!sees(sight, key0 + 16 * b + 4 * c4 + r)) s[b][r] = -INFINITY;
+    }
+    // ---- online softmax.  The running maximum m (common to the four lanes of
+    // a vector) moves only when the probabilities taken against it grow past
+    // 2^kLazy, or while it is -inf and the vector sees a key.
+    float p[8], big = -INFINITY, lt = 0.0f;
+    float mc = m == -INFINITY ? 0.0f : m * sc;
+#pragma unroll
+    for (int r = 0; r < 8; ++r) {
+      big = fmaxf(big, s[r >> 2][r & 3]);
+      p[r] = __builtin_amdgcn_exp2f(fmaf(s[r >> 2][r & 3], sc, -mc));
+      lt += p[r];
+    }
+    if (__builtin_amdgcn_ballot_w64(!(lt <= kLazySum) || (m == -INFINITY && big > -INFINITY))) {
+      big = fmaxf(big, __shfl_xor(big, 16));
+      big = fmaxf(big, __shfl_xor(big, 32));
+      const float mn = fmaxf(m, big);
+      const float alpha = mn == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f((m - mn) * sc);
+      m = mn;
+      l *= alpha;
+#pragma unroll
+      for (int db = 0; db < 8; ++db) o[db] *= alpha;
+      mc = m == -INFINITY ? 0.0f : m * sc;
+      lt = 0.0f;
+#pragma unroll
+      for (int r = 0; r < 8; ++r) {
+        p[r] = __builtin_amdgcn_exp2f(fmaf(s[r >> 2][r & 3], sc, -mc));
+        lt += p[r];
+      }
+    }
+    l += lt;
+    bf16x8 ph, pl;
+#pragma unroll
+    for (int r = 0; r < 8; ++r) {
+      ph[r] = (__bf16)p[r];
+      pl[r] = (__bf16)(p[r] - (float)ph[r]);
+    }
+    // ---- O^T += V^T P^T
+    const uint32_t va = lds_addr(vrows) + toff;
+    Frag vf[8];
+    // (LDS keeps a wave's accesses in order; this keeps the compiler to it)
+    if constexpr (F4) asm volatile("" ::: "memory");
+#pragma unroll
+    for (int db = 0; db < 8; ++db)
+#pragma unroll
+      for (int b = 0; b < 2; ++b) {
+        const s16x4 x = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+            (lds_s16x4*)(uintptr_t)((va ^ (32 * db)) + 4096 * b));
+        const uint2 u = __builtin_bit_cast(uint2, x);
+        vf[db].w[2 * b] = u.x;
+        vf[db].w[2 * b + 1] = u.y;
+      }
+    // A masked key weighs 0, but 0 x inf is not 0: where a masked tile's V is
+    // not finite everywhere, each vector adds the keys it sees one by one.
+    bool plain = true;
+    if (masked) {
+      uint32_t bad = 0;
+#pragma unroll
+      for (int db = 0; db < 8; ++db)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const uint32_t x = vf[db].w[e] & 0x7f807f80u;
+          bad |= ((x & 0xffff0000u) == 0x7f800000u) | ((x & 0xffffu) == 0x7f80u);
+        }
+      plain = __builtin_amdgcn_ballot_w64(bad != 0) == 0;
+    }
+    if (plain) {
+#pragma unroll
+      for (int db = 0; db < 8; ++db) {
+        o[db] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf[db].b, ph, o[db], 0, 0, 0);
+        o[db] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf[db].b, pl, o[db], 0, 0, 0);
+      }
+    } else {
+#pragma unroll 1
+      for (int j = 0; j < kStepKeys; ++j) {
+        float pj = 0.0f;
+#pragma unroll
+        for (int r = 0; r < 8; ++r)
+          if (r == 4 * (j >> 4) + (j & 3)) pj = p[r];
+        pj = __shfl(pj, 16 * ((j >> 2) & 3) + c16);
+        if (!sees(sight, key0 + j)) continue;
+#pragma unroll
+        for (int db = 0; db < 8; ++db) {
+          const uint2 u = *reinterpret_cast<const uint2*>(
+              vrows + j * (2 * kD) + 32 * (db ^ (j & 7)) + 8 * c4);
+          o[db][0] = fmaf(pj, bf16_to_f32(u.x & 0xffffu), o[db][0]);
+          o[db][1] = fmaf(pj, bf16_to_f32(u.x >> 16), o[db][1]);
+          o[db][2] = fmaf(pj, bf16_to_f32(u.y & 0xffffu), o[db][2]);
+          o[db][3] = fmaf(pj, bf16_to_f32(u.y >> 16), o[db][3]);
+        }
+      }
+    }
+  };
+
+  int stage = 0, ahead = ST - 1;
+  for (int i = 0; i < n; ++i) {
+    if (i + ST - 1 < n) {
+      wait_lds();   // the tile read from this buffer has been read
+      issue(i + ST - 1, ahead);
+      if (i + ST < n) fetch_pages(i + ST);
+      wait_vm<(ST - 1) * T::kLoads>();
+    } else {
+      wait_vm<0>();
+    }
+    tile(tile_key(i), mine + stage * T::kBytes);
+    stage = stage + 1 == ST ? 0 : stage + 1;
+    ahead = ahead + 1 == ST ? 0 : ahead + 1;
+  }
+  l += __shfl_xor(l, 16);
+  l += __shfl_xor(l, 32);
+
+  // ---- the waves join: weights 2^((m_w - M) c), M the vector's maximum
+  __syncthreads();
+  float* om = reinterpret_cast<float*>(lds);
+  float* st = om + NW * kStepVecs * kOStr;
+#pragma unroll
+  for (int db = 0; db < 8; ++db)
+    *reinterpret_cast<f32x4*>(om + (w * kStepVecs + c16) * kOStr + 16 * db + 4 * c4) = o[db];
+  if (c4 == 0) {
+    st[(w * kStepVecs + c16) * 2] = m;
+    st[(w * kStepVecs + c16) * 2 + 1] = l;
+  }
+  __syncthreads();
+  const int vec = tid >> 4, d0 = 8 * (tid & 15);
+  const int r = vec / it.n_heads, h = vec - r * it.n_heads;
+  if (r >= it.n_rows) return;
+  float M = -INFINITY, L = 0.0f, acc[8] = {};
+#pragma unroll
+  for (int x = 0; x < NW; ++x) M = fmaxf(M, st[(x * kStepVecs + vec) * 2]);
+#pragma unroll
+  for (int x = 0; x < NW; ++x) {
+    const float mx = st[(x * kStepVecs + vec) * 2];
+    const float wt = mx == M && M == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f((mx - M) * sc);
+    L = fmaf(wt, st[(x * kStepVecs + vec) * 2 + 1], L);
+    const float* src = om + (x * kStepVecs + vec) * kOStr + d0;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) acc[e] = fmaf(wt, src[e], acc[e]);
+  }
+  const int64_t orow = (int64_t)(it.row0 + r) * a.n_q_heads + it.kv_head * G + it.head0 + h;
+  float ls = M * a.scale + logf(L);
+  if (it.part_slot >= 0) {
+    // a range without a key the row sees (or all of its scores -inf) weighs
+    // nothing: 0, -inf
+    const bool none = L == 0.0f;
+    const float inv = none ? 0.0f : 1.0f / L;
+    float* po = a.split_o + ((int64_t)it.part_slot * kStepVecs + vec) * kD + d0;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) acc[e] *= inv;
+    store8(po, acc);
+    if (d0 == 0) a.split_lse[(int64_t)it.part_slot * kStepVecs + vec] = none ? -INFINITY : ls;
+    return;
+  }
+  const StepRow row = a.rows[it.row0 + r];
+  const bool empty = row.pos < 0 || row.lo > row.pos;
+  const float inv = 1.0f / L;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) acc[e] = empty ? 0.0f : acc[e] * inv;
+  store8(static_cast<uint16_t*>(a.out) + orow * kD + d0, acc);
+  if (a.lse && d0 == 0) a.lse[orow] = empty ? -INFINITY : ls;
+}
+
+// ------------------------------------------------------------- fp32 pages
+// The reference mode, as for composed prefills: fp32 operands, fp64 products,
+// softmax and sums, one rounding.  Item, lanes and joining as above with
+// v_mfma_f64_16x16x4_f64: lane l holds query vector (or key) l % 16 and the
+// dims of quarter l / 16; result register r is key 4 r + l / 16.
+typedef double f64x4 __attribute__((ext_vector_type(4)));
+
+template <int D>
+__global__ __launch_bounds__(64 * kStepWaves) void step_attn_f32_kernel(const StepAttnArgs a) {
+  constexpr int NW = kStepWaves, DQ = D / 4, DT = D / 16, kRound = 4;
+  __shared__ double om[NW][16 * kRound][kStepVecs];
+  __shared__ double ml[2][NW][kStepVecs];
+  const StepItem it = a.items[blockIdx.x];
+  if (it.n_rows == 0) return;
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int c16 = lane & 15, c4 = lane >> 4;
+  const int G = a.n_q_heads / a.n_kv_heads;
+  const int page_mask = (1 << a.log2_page) - 1;
+  const int32_t* bt = a.bts + it.bt_off;
+  int vr = c16 / it.n_heads, vh = c16 - vr * it.n_heads;
+  const bool real = vr < it.n_rows;
+  if (!real) vr = vh = 0;
+  const StepRow row = a.rows[it.row0 + vr];
+  const Sight sight = row_sight(row, a.window, a.n_sinks);
+  const int64_t orow =
+      (int64_t)(it.row0 + vr) * a.n_q_heads + it.kv_head * G + it.head0 + vh;
+  float qr[DQ];
+  {
+    const float* qp = static_cast<const float*>(a.q) + orow * D + DQ * c4;
+#pragma unroll
+    for (int e = 0; e < DQ; e += 4) {
+      const float4 x = *reinterpret_cast<const float4*>(qp + e);
+      qr[e] = x.x;
+      qr[e + 1] = x.y;
+      qr[e + 2] = x.z;
+      qr[e + 3] = x.w;
+    }
+  }
+  f64x4 o[DT];
+#pragma unroll
+  for (int t = 0; t < DT; ++t) o[t] = f64x4{0.0, 0.0, 0.0, 0.0};
+  double m = -INFINITY, l = 0.0;
+  const double sc = a.scale;
+  auto key_base = [&](int k) -> int64_t {   // keys past the last one read it
+    const int kk = min(k, it.kv_len - 1);
+    return ((((int64_t)bt[kk >> a.log2_page] * a.n_kv_heads + it.kv_head) << a.log2_page) +
+            (kk & page_mask)) * D;
+  };
+  const float* kc = static_cast<const float*>(a.k);
+  const float* vc = static_cast<const float*>(a.v);
+  // 16-key halves of the item's tiles
+  const int na = 2 * (it.a1 - it.a0), nt = na + 2 * (it.b1 - it.b0);
+  for (int i = w; i < nt; i += NW) {
+    const int k0 = 16 * (i < na ? 2 * it.a0 + i : 2 * it.b0 + i - na);
+    const float* kp = kc + key_base(k0 + c16) + DQ * c4;
+    const float* vp[4];
+#pragma unroll
+    for (int r = 0; r < 4; ++r) vp[r] = vc + key_base(k0 + 4 * r + c4) + c16;
+    f64x4 s = {0.0, 0.0, 0.0, 0.0};
+#pragma unroll
+    for (int e = 0; e < DQ; e += 4) {
+      const float4 x = *reinterpret_cast<const float4*>(kp + e);
+      s = __builtin_amdgcn_mfma_f64_16x16x4f64(x.x, qr[e], s, 0, 0, 0);
+      s = __builtin_amdgcn_mfma_f64_16x16x4f64(x.y, qr[e + 1], s, 0, 0, 0);
+      s = __builtin_amdgcn_mfma_f64_16x16x4f64(x.z, qr[e + 2], s, 0, 0, 0);
+      s = __builtin_amdgcn_mfma_f64_16x16x4f64(x.w, qr[e + 3], s, 0, 0, 0);
+    }
+    const bool masked = k0 < it.full_lo || k0 + 15 > it.full_hi;
+    double mt = -INFINITY;
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      s[r] = !masked || sees(sight, k0 + 4 * r + c4) ? s[r] * sc : -INFINITY;
+      mt = fmax(mt, s[r]);
+    }
+    mt = fmax(mt, __shfl_xor(mt, 16));
+    mt = fmax(mt, __shfl_xor(mt, 32));
+    const double mn = fmax(m, mt);
+    const double mb = mn == -INFINITY ? 0.0 : mn;   // no key seen yet
+    const double alpha = exp(m - mb);
+    m = mn;
+    double p[4], ps = 0.0;
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      p[r] = exp(s[r] - mb);
+      ps += p[r];
+    }
+    l = l * alpha + ps;
+#pragma unroll
+    for (int t = 0; t < DT; ++t)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) o[t][r] *= alpha;
+    // as in the bf16 kernel: 0 x inf is not 0
+    bool plain = true;
+    if (masked) {
+      float z = 0.0f;
+#pragma unroll
+      for (int r = 0; r < 4; ++r)
+#pragma unroll
+        for (int t = 0; t < DT; ++t) z = fmaf(vp[r][16 * t], 0.0f, z);
+      plain = __builtin_amdgcn_ballot_w64(z != 0.0f) == 0;
+    }
+    if (plain) {
+#pragma unroll
+      for (int r = 0; r < 4; ++r)
+#pragma unroll
+        for (int t = 0; t < DT; ++t)
+          o[t] = __builtin_amdgcn_mfma_f64_16x16x4f64((double)vp[r][16 * t], p[r], o[t], 0, 0, 0);
+    } else {
+#pragma unroll 1
+      for (int j = 0; j < 16; ++j) {
+        const double pr = j < 8 ? (j < 4 ? p[0] : p[1]) : (j < 12 ? p[2] : p[3]);
+        const double pj = __shfl(pr, 16 * (j % 4) + c16);
+        if (!sees(sight, k0 + j)) continue;
+        const float* vj = vc + key_base(k0 + j) + c4;
+#pragma unroll
+        for (int t = 0; t < DT; ++t)
+#pragma unroll
+          for (int r = 0; r < 4; ++r)
+            o[t][r] = fma(pj, (double)vj[16 * t + 4 * r], o[t][r]);
+      }
+    }
+  }
+  l += __shfl_xor(l, 16);
+  l += __shfl_xor(l, 32);
+  if (c4 == 0) {
+    ml[0][w][c16] = m;
+    ml[1][w][c16] = l;
+  }
+  __syncthreads();
+  double M = -INFINITY, L = 0.0;
+#pragma unroll
+  for (int x = 0; x < NW; ++x) M = fmax(M, ml[0][x][c16]);
+  auto weight = [&](double mx) { return mx == M && M == -INFINITY ? 1.0 : exp(mx - M); };
+#pragma unroll
+  for (int x = 0; x < NW; ++x) L += ml[1][x][c16] * weight(ml[0][x][c16]);
+  const bool empty = row.pos < 0 || row.lo > row.pos;
+  const bool part = it.part_slot >= 0;
+  const bool zero = part ? L == 0.0 : empty;
+  const double wt = weight(m) / L;
+  for (int t0 = 0; t0 < DT; t0 += kRound) {
+    if (t0) __syncthreads();
+#pragma unroll
+    for (int t = 0; t < DT; ++t)
+      if (t / kRound * kRound == t0)
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+          om[w][16 * (t - t0) + 4 * r + c4][c16] = zero ? 0.0 : o[t][r] * wt;
+    __syncthreads();
+    for (int i = tid; i < 16 * kRound * kStepVecs; i += 64 * NW) {
+      const int d = i % (16 * kRound), vec = i / (16 * kRound);
+      const int r = vec / it.n_heads, h = vec - r * it.n_heads;
+      if (r >= it.n_rows) continue;
+      double sum = 0.0;
+#pragma unroll
+      for (int x = 0; x < NW; ++x) sum += om[x][d][vec];
+      const int64_t to = (int64_t)(it.row0 + r) * a.n_q_heads + it.kv_head * G + it.head0 + h;
+      if (part)
+        a.split_o[((int64_t)it.part_slot * kStepVecs + vec) * D + 16 * t0 + d] = (float)sum;
+      else
+        static_cast<float*>(a.out)[to * D + 16 * t0 + d] = (float)sum;
+    }
+  }
+  if (w == 0 && c4 == 0 && real) {
+    const float ls = zero ? -INFINITY : (float)(M + log(L));
+    if (part)
+      a.split_lse[(int64_t)it.part_slot * kStepVecs + c16] = ls;
+    else if (a.lse)
+      a.lse[orow] = ls;
+  }
+}
+
+// ------------------------------------------------------------ key ranges
+// lse = log sum_c exp(lse_c), o = sum_c exp(lse_c - lse) o_c over an item's
+// ranges c, in their order.  Half a wave takes a vector, D / 32 dims a lane;
+// lane c % 32 holds the weight of range c.
+struct MergeArgs {
+  const StepRow* rows;
+  const StepMerge* merges;
+  const float *split_o, *split_lse;
+  void* out;
+  float* lse;
+  int32_t n_q_heads;
+};
+constexpr int kMergeVecs = 8;   // of a workgroup of 256
+constexpr int kMergeAhead = 8;
+
+template <typename E, int D>
+__global__ __launch_bounds__(256) void step_merge_kernel(const MergeArgs a) {
+  constexpr int W = D / 32;
+  typedef float vec_t __attribute__((ext_vector_type(W)));
+  const StepMerge g = a.merges[blockIdx.x];
+  const int lane = threadIdx.x & 31;
+  const int vec = blockIdx.y * kMergeVecs + (threadIdx.x >> 5);
+  const int r = vec / g.n_heads, h = vec - r * g.n_heads;
+  if (r >= g.n_rows) return;
+  auto at = [&](int c) { return (int64_t)(g.slot0 + c) * kStepVecs + vec; };
+  auto part = [&](int c) {
+    return *reinterpret_cast<const vec_t*>(a.split_o + at(c) * D + W * lane);
+  };
+  auto range_lse = [&](int c) { return c < g.n_slots ? a.split_lse[at(c)] : -INFINITY; };
+  const float l0 = range_lse(lane);
+  const StepRow row = a.rows[g.row0 + r];
+  vec_t ahead[kMergeAhead];   // past the last range: it again, unused
+#pragma unroll
+  for (int c = 0; c < kMergeAhead; ++c) ahead[c] = part(min(c, g.n_slots - 1));
+  float mx = l0;
+  for (int c = lane + 32; c < g.n_slots; c += 32) mx = fmaxf(mx, range_lse(c));
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) mx = fmaxf(mx, __shfl_xor(mx, o));
+  float den = expf(l0 - mx);
+  for (int c = lane + 32; c < g.n_slots; c += 32) den += expf(range_lse(c) - mx);
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) den += __shfl_xor(den, o);
+  const float inv = 1.0f / den;
+  vec_t acc = 0.0f;
+  float wl = expf(l0 - mx) * inv;
+#pragma unroll
+  for (int c = 0; c < kMergeAhead; ++c) {
+    const float wc = __shfl(wl, c, 32);
+    if (c < g.n_slots) acc += wc * ahead[c];
+  }
+  for (int c = kMergeAhead; c < g.n_slots; ++c) {
+    if (c % 32 == 0) wl = expf(range_lse(c + lane) - mx) * inv;
+    acc += __shfl(wl, c % 32, 32) * part(c);
+  }
+  const bool empty = row.pos < 0 || row.lo > row.pos;
+  if (empty) acc = 0.0f;
+  const int64_t to = (int64_t)(g.row0 + r) * a.n_q_heads + g.hq0 + h;
+  E* dst = static_cast<E*>(a.out) + to * D + W * lane;
+#pragma unroll
+  for (int e = 0; e < W; ++e) {
+    if constexpr (sizeof(E) == 2)
+      dst[e] = (E)f32_to_bf16(acc[e]);
+    else
+      dst[e] = acc[e];
+  }
+  if (a.lse) {
+    float ls = mx + logf(den);
+    if (mx == -INFINITY) {   // every range -inf, or NaN
+      ls = 0.0f;
+      for (int c = 0; c < g.n_slots; ++c) ls += a.split_lse[at(c)];
+    }
+    if (lane == 0) a.lse[to] = empty ? -INFINITY : ls;
+  }
+}
+
+int ilog2(int x) {
+  int l = 0;
+  while ((1 << l) < x) ++l;
+  return l;
+}
+
+}  // namespace
+
+hipError_t launch_step_attn(const tsr_step* p, const void* q, const void* req_k,
+                            const void* req_v, const void* req_scale, void* out, float* lse,
+                            hipStream_t s) {
+  const tsr_model& m = p->model;
+  StepAttnArgs a{};
+  a.rows = p->dev.rows;
+  a.items = p->dev.items;
+  a.bts = p->dev.bts;
+  a.q = q;
+  a.k = req_k;
+  a.v = req_v;
+  a.scales = static_cast<const uint8_t*>(req_scale);
+  a.out = out;
+  a.lse = lse;
+  a.split_o = p->dev.split_o;
+  a.split_lse = p->dev.split_lse;
+  a.n_q_heads = m.n_q_heads;
+  a.n_kv_heads = m.n_kv_heads;
+  a.log2_page = ilog2(m.page_size);
+  a.window = p->opt.window;
+  a.n_sinks = p->opt.n_sinks;
+  a.scale = p->scale;
+  a.scale_log2e = (float)((double)p->scale * 1.4426950408889634);
+  const dim3 grid(p->n_items), block(64 * kStepWaves);
+  MergeArgs g{p->dev.rows, p->dev.merges, p->dev.split_o, p->dev.split_lse, out, lse,
+              m.n_q_heads};
+  const dim3 mgrid(p->n_merges, kStepVecs / kMergeVecs);
+#define TSR_STEP(KERNEL, E, D)                                               \
+  do {                                                                       \
+    hipLaunchKernelGGL(KERNEL, grid, block, 0, s, a);                        \
+    hipError_t e = hipGetLastError();                                        \
+    if (e != hipSuccess || p->n_merges == 0) return e;                       \
+    hipLaunchKernelGGL((step_merge_kernel<E, D>), mgrid, dim3(256), 0, s, g); \
+    return hipGetLastError();                                                \
+  } while (0)
+  if (m.kv_dtype == TSR_BF16) TSR_STEP((step_attn_kernel<false>), uint16_t, kD);
+  if (m.kv_dtype == TSR_E2M1) TSR_STEP((step_attn_kernel<true>), uint16_t, kD);
+  switch (m.head_dim) {
+    case 64: TSR_STEP((step_attn_f32_kernel<64>), float, 64);
+    case 128: TSR_STEP((step_attn_f32_kernel<128>), float, 128);
+    case 256: TSR_STEP((step_attn_f32_kernel<256>), float, 256);
+    default: return hipErrorInvalidValue;
+  }
+#undef TSR_STEP
+}
+
+}  // namespace tsr

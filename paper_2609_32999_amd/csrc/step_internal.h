@@ -1,0 +1,112 @@
+// Internal declarations of the steps of tsr_step.h: the device image of a
+// step and the kernel launchers.  Not part of the ABI.
+#pragma once
+
+#include <hip/hip_runtime.h>
+
+#include <cstdint>
+#include <vector>
+
+#include "../../include/tsr_step.h"
+#include "tsr_internal.h"
+
+namespace tsr {
+
+// Rows of an attention item times the query heads it takes: one operand of
+// a 16 x 16 matrix instruction (kernel for few rows).
+constexpr int kStepVecs = 16;
+// Keys per tile: two 16-key blocks, each within one page (bf16, e2m1).
+constexpr int kStepKeys = 32;
+
+// A row: its position (-1: no token), first visible key and, as an append
+// target, the slot page * page_size + slot-in-page of its position.
+struct alignas(16) StepRow {
+  int32_t pos;
+  int32_t lo;
+  int32_t dst;
+  int32_t pad;
+};
+
+// Attention work item: rows row0 .. row0 + n_rows - 1 (one request), query
+// heads head0 .. head0 + n_heads - 1 of KV head kv_head, over the key tiles
+// [a0, a1) and [b0, b1) (sinks and window; or one range of them).  n_rows ==
+// 0 marks padding.  Keys in [full_lo, full_hi] are visible to every row.
+struct alignas(16) StepItem {
+  int32_t row0;
+  int32_t n_rows;
+  int32_t kv_head;
+  int32_t head0;      // within the KV head's group
+  int32_t n_heads;
+  int32_t bt_off;     // the request's block table
+  int32_t kv_len;
+  int32_t a0, a1, b0, b1;
+  int32_t full_lo, full_hi;
+  int32_t part_slot;  // -1: writes out and lse, else its split buffer slot
+  int32_t pad[2];
+};
+
+// A split item: its ranges are slots slot0 .. slot0 + n_slots - 1.
+struct alignas(16) StepMerge {
+  int32_t row0;
+  int32_t n_rows;
+  int32_t hq0;       // first query head
+  int32_t n_heads;
+  int32_t slot0;
+  int32_t n_slots;
+  int32_t pad[2];
+};
+
+// A page of the requests and how many of its slots hold positions.
+struct alignas(8) StepPage {
+  int32_t page;
+  int32_t n;
+};
+
+struct StepDev {
+  const StepRow* rows;
+  const StepItem* items;
+  const StepMerge* merges;
+  const StepPage* pages;
+  const int32_t* bts;
+  float* split_o;    // [slots][vecs][head_dim], normalised
+  float* split_lse;  // [slots][vecs], natural log
+  const float* rope_cos;
+  const float* rope_sin;
+};
+
+}  // namespace tsr
+
+struct tsr_step {
+  tsr_model model;
+  tsr_step_options opt;
+  float scale;
+  int32_t T, n_items, n_merges, n_pages, n_req_pages;
+  int32_t item_vecs;       // rows x heads of an item
+  bool shared_append;      // a row's page belongs to another request too
+  size_t image_bytes, ws_bytes;
+  size_t off_rows, off_items, off_merges, off_pages, off_bts, off_split_o, off_split_lse;
+  std::vector<char> image;
+  void* ws;
+  tsr::StepDev dev;
+};
+
+namespace tsr {
+
+// The checks common to every model (heads, page size, RoPE, scale).
+tsr_status check_model_fields(const tsr_model* m);
+// A model that steps take.
+tsr_status check_step_model(const tsr_model* m);
+
+hipError_t launch_step_append(const tsr_step* p, const tsr_qk_norm* norm, const void* q,
+                              int64_t q_stride, const void* k, int64_t k_stride, const void* v,
+                              int64_t v_stride, void* q_out, void* k_pre, void* req_k,
+                              void* req_v, void* req_scale, hipStream_t s);
+hipError_t launch_step_pack(const tsr_step* p, const void* bf16_k, const void* bf16_v,
+                            void* req_k, void* req_v, void* req_scale, hipStream_t s);
+hipError_t launch_step_unpack(const tsr_step* p, const void* req_k, const void* req_v,
+                              const void* req_scale, void* bf16_k, void* bf16_v, hipStream_t s);
+hipError_t launch_step_attn(const tsr_step* p, const void* q, const void* req_k,
+                            const void* req_v, const void* req_scale, void* out, float* lse,
+                            hipStream_t s);
+
+}  // namespace tsr

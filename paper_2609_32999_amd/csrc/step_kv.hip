@@ -1,0 +1,296 @@
+// KV movement of the steps (tsr_step.h):
+//   append   norms of query and key heads, RoPE, page write, in one pass;
+//   pack     bf16 pages -> 4-bit pages;
+//   unpack   4-bit pages -> bf16 pages.
+// All three read each input once and write each output once.
+#include "e2m1.h"
+#include "kernels_common.h"
+#include "step_internal.h"
+
+namespace tsr {
+
+namespace {
+
+enum PageKind { kPageF32, kPageBf16, kPageE2m1 };
+
+struct AppendArgs {
+  const StepRow* rows;
+  const void *q, *k, *v, *q_weight, *k_weight;
+  void *q_out, *k_pre, *req_k, *req_v;
+  uint8_t* req_scale;
+  const float *rope_cos, *rope_sin;
+  int64_t q_stride, k_stride, v_stride;
+  int32_t T, n_q_heads, n_kv_heads, log2_page, units;
+  float eps;
+  bool norm;
+};
+
+// One block of 32 dims of a head, 8 of them in each of four lanes, as codes
+// and a scale byte.  `at`: the head's element offset / 32 in the pages.
+__device__ __forceinline__ void put_e2m1(const float* x, int c, int block, int64_t head,
+                                         uint8_t* codes, uint8_t* scale) {
+  float amax = 0.0f;
+  bool finite = true;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    amax = fmaxf(amax, fabsf(x[i]));
+    finite = finite && fabsf(x[i]) <= 3.402823466e38f;
+  }
+  int ok = finite;
+#pragma unroll
+  for (int o = 1; o < 4; o <<= 1) {
+    amax = fmaxf(amax, __shfl_xor(amax, o));
+    ok &= __shfl_xor(ok, o);
+  }
+  const uint32_t b = e2m1_scale(amax, ok);
+  *reinterpret_cast<uint32_t*>(codes + head * 64 + 16 * block + 4 * (c & 3)) =
+      e2m1_encode8(x, e2m1_factor(b));
+  if ((c & 3) == 0) scale[block] = (uint8_t)b;
+}
+
+// A group of D / 16 lanes takes one head vector: lane c holds dims 8 c .. and
+// D/2 + 8 c .., the two members of eight RoPE pairs, so that the norm is
+// one sum over the group and the rotation stays in the lane.  The group's N
+// vectors are of one row (heads j, j + units, ...: query heads, then key and
+// value heads), so its cos and sin are read once.
+template <typename E, int KIND, int D, int N>
+__global__ __launch_bounds__(256) void step_append_kernel(const AppendArgs a) {
+  constexpr int L = D / 16, H = D / 2;
+  const int c = threadIdx.x % L;
+  const int64_t grp = (int64_t)blockIdx.x * (256 / L) + threadIdx.x / L;
+  const int64_t t64 = grp / a.units;
+  if (t64 >= a.T) return;   // whole groups leave together
+  const int t = (int)t64, j = (int)(grp % a.units);
+  const int nq = a.n_q_heads, nk = a.n_kv_heads, n_vec = nq + 2 * nk;
+  const StepRow row = a.rows[t];
+  if (row.pos < 0) return;
+
+  float x[N][16];
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    const int h = j + i * a.units;
+    if (h >= n_vec) break;
+    const E* src = h < nq        ? static_cast<const E*>(a.q) + t * a.q_stride + (int64_t)h * D
+                   : h < nq + nk ? static_cast<const E*>(a.k) + t * a.k_stride + (int64_t)(h - nq) * D
+                                 : static_cast<const E*>(a.v) + t * a.v_stride +
+                                       (int64_t)(h - nq - nk) * D;
+    load8(src + 8 * c, x[i]);
+    load8(src + H + 8 * c, x[i] + 8);
+  }
+  float cs[8], sn[8];
+  load8(a.rope_cos + (int64_t)row.pos * H + 8 * c, cs);
+  load8(a.rope_sin + (int64_t)row.pos * H + 8 * c, sn);
+
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    const int h = j + i * a.units;
+    if (h >= n_vec) break;
+    const bool is_q = h < nq, is_v = h >= nq + nk;
+    const int g = h - nq - (is_v ? nk : 0);       // KV head
+    if (!is_v) {
+      if (a.norm) {
+        float s = 0.0f;
+#pragma unroll
+        for (int e = 0; e < 16; ++e) s = fmaf(x[i][e], x[i][e], s);
+#pragma unroll
+        for (int o = 1; o < L; o <<= 1) s += __shfl_xor(s, o);
+        const float r = 1.0f / sqrtf(s * (1.0f / D) + a.eps);
+        const E* w = static_cast<const E*>(is_q ? a.q_weight : a.k_weight);
+        if (w) {
+          float wv[16];
+          load8(w + 8 * c, wv);
+          load8(w + H + 8 * c, wv + 8);
+#pragma unroll
+          for (int e = 0; e < 16; ++e) x[i][e] = x[i][e] * r * wv[e];
+        } else {
+#pragma unroll
+          for (int e = 0; e < 16; ++e) x[i][e] *= r;
+        }
+      }
+      if (!is_q) {
+        // the form a unit cache keeps; K is rotated from it, so that a unit
+        // composed from the cache holds the same bits
+        if constexpr (sizeof(E) == 2) {
+#pragma unroll
+          for (int e = 0; e < 16; ++e) x[i][e] = bf16_to_f32(f32_to_bf16(x[i][e]));
+        }
+        if (a.k_pre) {
+          E* dst = static_cast<E*>(a.k_pre) + ((int64_t)t * nk + g) * D;
+          store8(dst + 8 * c, x[i]);
+          store8(dst + H + 8 * c, x[i] + 8);
+        }
+      }
+      rope_rotate<8>(x[i], x[i] + 8, cs, sn);
+    }
+    if (is_q) {
+      E* dst = static_cast<E*>(a.q_out) + ((int64_t)t * nq + h) * D;
+      store8(dst + 8 * c, x[i]);
+      store8(dst + H + 8 * c, x[i] + 8);
+      continue;
+    }
+    const int64_t head = ((((int64_t)(row.dst >> a.log2_page) * nk + g) << a.log2_page) +
+                          (row.dst & ((1 << a.log2_page) - 1)));
+    void* pages = is_v ? a.req_v : a.req_k;
+    if constexpr (KIND == kPageE2m1) {
+      const int64_t page = row.dst >> a.log2_page;
+      const int64_t sc = ((((page * 2 + is_v) * nk + g) << a.log2_page) +
+                          (row.dst & ((1 << a.log2_page) - 1)));
+      uint8_t* scale = a.req_scale + sc * (D / kScaleDims);
+      put_e2m1(x[i], c, c / 4, head, static_cast<uint8_t*>(pages), scale);
+      put_e2m1(x[i] + 8, c, D / 64 + c / 4, head, static_cast<uint8_t*>(pages), scale);
+    } else {
+      E* dst = static_cast<E*>(pages) + head * D;
+      store8(dst + 8 * c, x[i]);
+      store8(dst + H + 8 * c, x[i] + 8);
+    }
+  }
+}
+
+template <typename E, int KIND, int D>
+hipError_t run_append(AppendArgs a, hipStream_t s) {
+  const int n_vec = a.n_q_heads + 2 * a.n_kv_heads;
+  auto blocks = [&](int units) {
+    return (unsigned)(((int64_t)a.T * units + 256 / (D / 16) - 1) / (256 / (D / 16)));
+  };
+  constexpr int N = 4;
+  a.units = (n_vec + N - 1) / N;
+  if (blocks(a.units) >= 4 * kNumCus) {
+    hipLaunchKernelGGL((step_append_kernel<E, KIND, D, N>), dim3(blocks(a.units)), dim3(256), 0, s,
+                       a);
+  } else {
+    a.units = n_vec;
+    hipLaunchKernelGGL((step_append_kernel<E, KIND, D, 1>), dim3(blocks(a.units)), dim3(256), 0, s,
+                       a);
+  }
+  return hipGetLastError();
+}
+
+constexpr int kD4 = 128;   // head dim of 4-bit pages
+
+// Lane: 16 dims of a slot; a workgroup: one page of K (blockIdx.y 0) or V.
+__global__ __launch_bounds__(256) void step_pack_kernel(
+    const StepPage* __restrict__ pages, const uint16_t* __restrict__ src_k,
+    const uint16_t* __restrict__ src_v, uint8_t* __restrict__ dst_k, uint8_t* __restrict__ dst_v,
+    uint8_t* __restrict__ scales, int n_kv_heads, int log2_page) {
+  const StepPage pg = pages[blockIdx.x];
+  const int is_v = blockIdx.y;
+  const int n = (n_kv_heads << log2_page) * (kD4 / 16);
+  const int64_t first = ((int64_t)pg.page * n_kv_heads) << log2_page;
+  const uint16_t* src = (is_v ? src_v : src_k) + first * kD4;
+  uint8_t* dst = (is_v ? dst_v : dst_k) + first * (kD4 / 2);
+  uint8_t* scale = scales + (2 * first + (is_v ? (int64_t)n_kv_heads << log2_page : 0)) *
+                                (kD4 / kScaleDims);
+  for (int i = threadIdx.x; i < n; i += 256) {
+    if (((i >> 3) & ((1 << log2_page) - 1)) >= pg.n) continue;   // 8 lanes a slot
+    float x[16];
+    load8(src + (int64_t)i * 16, x);
+    load8(src + (int64_t)i * 16 + 8, x + 8);
+    float amax = 0.0f;
+    int ok = 1;
+#pragma unroll
+    for (int e = 0; e < 16; ++e) {
+      amax = fmaxf(amax, fabsf(x[e]));
+      ok &= fabsf(x[e]) <= 3.402823466e38f;
+    }
+    amax = fmaxf(amax, __shfl_xor(amax, 1));
+    ok &= __shfl_xor(ok, 1);
+    const uint32_t b = e2m1_scale(amax, ok);
+    const float f = e2m1_factor(b);
+    *reinterpret_cast<uint2*>(dst + (int64_t)i * 8) =
+        make_uint2(e2m1_encode8(x, f), e2m1_encode8(x + 8, f));
+    if ((i & 1) == 0) scale[i >> 1] = (uint8_t)b;
+  }
+}
+
+__global__ __launch_bounds__(256) void step_unpack_kernel(
+    const StepPage* __restrict__ pages, const uint8_t* __restrict__ src_k,
+    const uint8_t* __restrict__ src_v, const uint8_t* __restrict__ scales,
+    uint16_t* __restrict__ dst_k, uint16_t* __restrict__ dst_v, int n_kv_heads, int log2_page) {
+  const StepPage pg = pages[blockIdx.x];
+  const int is_v = blockIdx.y;
+  const int n = (n_kv_heads << log2_page) * (kD4 / 16);
+  const int64_t first = ((int64_t)pg.page * n_kv_heads) << log2_page;
+  const uint8_t* src = (is_v ? src_v : src_k) + first * (kD4 / 2);
+  uint16_t* dst = (is_v ? dst_v : dst_k) + first * kD4;
+  const uint8_t* scale = scales + (2 * first + (is_v ? (int64_t)n_kv_heads << log2_page : 0)) *
+                                      (kD4 / kScaleDims);
+  for (int i = threadIdx.x; i < n; i += 256) {
+    if (((i >> 3) & ((1 << log2_page) - 1)) >= pg.n) continue;
+    const uint2 c = *reinterpret_cast<const uint2*>(src + (int64_t)i * 8);
+    const float f = e2m1_factor(scale[i >> 1]);
+    uint4* d = reinterpret_cast<uint4*>(dst + (int64_t)i * 16);
+    d[0] = e2m1_decode8(c.x, f);
+    d[1] = e2m1_decode8(c.y, f);
+  }
+}
+
+int ilog2(int x) {
+  int l = 0;
+  while ((1 << l) < x) ++l;
+  return l;
+}
+
+}  // namespace
+
+hipError_t launch_step_append(const tsr_step* p, const tsr_qk_norm* norm, const void* q,
+                              int64_t q_stride, const void* k, int64_t k_stride, const void* v,
+                              int64_t v_stride, void* q_out, void* k_pre, void* req_k,
+                              void* req_v, void* req_scale, hipStream_t s) {
+  const tsr_model& m = p->model;
+  AppendArgs a{};
+  a.rows = p->dev.rows;
+  a.q = q;
+  a.k = k;
+  a.v = v;
+  a.q_out = q_out;
+  a.k_pre = k_pre;
+  a.req_k = req_k;
+  a.req_v = req_v;
+  a.req_scale = static_cast<uint8_t*>(req_scale);
+  a.rope_cos = p->dev.rope_cos;
+  a.rope_sin = p->dev.rope_sin;
+  a.q_stride = q_stride;
+  a.k_stride = k_stride;
+  a.v_stride = v_stride;
+  a.T = p->T;
+  a.n_q_heads = m.n_q_heads;
+  a.n_kv_heads = m.n_kv_heads;
+  a.log2_page = ilog2(m.page_size);
+  if (norm) {
+    a.norm = true;
+    a.eps = norm->eps;
+    a.q_weight = norm->q_weight;
+    a.k_weight = norm->k_weight;
+  }
+  if (m.kv_dtype == TSR_E2M1) return run_append<uint16_t, kPageE2m1, kD4>(a, s);
+  if (m.kv_dtype == TSR_BF16) return run_append<uint16_t, kPageBf16, 128>(a, s);
+  switch (m.head_dim) {
+    case 64: return run_append<float, kPageF32, 64>(a, s);
+    case 128: return run_append<float, kPageF32, 128>(a, s);
+    case 256: return run_append<float, kPageF32, 256>(a, s);
+    default: return hipErrorInvalidValue;
+  }
+}
+
+hipError_t launch_step_pack(const tsr_step* p, const void* bf16_k, const void* bf16_v,
+                            void* req_k, void* req_v, void* req_scale, hipStream_t s) {
+  hipLaunchKernelGGL(step_pack_kernel, dim3(p->n_pages, 2), dim3(256), 0, s, p->dev.pages,
+                     static_cast<const uint16_t*>(bf16_k), static_cast<const uint16_t*>(bf16_v),
+                     static_cast<uint8_t*>(req_k), static_cast<uint8_t*>(req_v),
+                     static_cast<uint8_t*>(req_scale), p->model.n_kv_heads,
+                     ilog2(p->model.page_size));
+  return hipGetLastError();
+}
+
+hipError_t launch_step_unpack(const tsr_step* p, const void* req_k, const void* req_v,
+                              const void* req_scale, void* bf16_k, void* bf16_v,
+                              hipStream_t s) {
+  hipLaunchKernelGGL(step_unpack_kernel, dim3(p->n_pages, 2), dim3(256), 0, s, p->dev.pages,
+                     static_cast<const uint8_t*>(req_k), static_cast<const uint8_t*>(req_v),
+                     static_cast<const uint8_t*>(req_scale), static_cast<uint16_t*>(bf16_k),
+                     static_cast<uint16_t*>(bf16_v), p->model.n_kv_heads,
+                     ilog2(p->model.page_size));
+  return hipGetLastError();
+}
+
+}  // namespace tsr

@@ -1,0 +1,498 @@
+// Steps of tsr_step.h on the host: validation, the row and attention item
+// lists, and the entry points.  Every check runs before anything is enqueued.
+#include <algorithm>
+#include <cmath>
+#include <cstring>
+#include <initializer_list>
+#include <memory>
+
+#include "step_internal.h"
+
+namespace tsr {
+
+namespace {
+
+size_t align_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
+
+tsr_status fail(tsr_status st, const std::string& msg) {
+  set_error(msg);
+  return st;
+}
+
+tsr_status fail_req(tsr_status st, int r, const std::string& msg) {
+  return fail(st, "request " + std::to_string(r) + ": " + msg);
+}
+
+// Compute units and key ranges: a launch is cut into about this many items
+// a compute unit, of kMinRangeTiles tiles at least.
+constexpr int kRangesPerCu = 2;
+constexpr int kMinRangeTiles = 8;
+constexpr int kMaxStepSlots = 1 << 16;
+
+// Key tiles [a0, a1) and [b0, b1) that hold every key some row of
+// rows[r0 .. r0 + n) sees, and the keys visible to all of them.
+void item_keys(const std::vector<StepRow>& rows, int r0, int n, const tsr_step_options& o,
+               StepItem* it) {
+  constexpr int64_t kNone = INT32_MAX;
+  int64_t s_lo = kNone, s_hi = 0, w_lo = kNone, w_hi = 0, f_lo = 0, f_hi = kNone;
+  for (int i = r0; i < r0 + n; ++i) {
+    const StepRow& r = rows[i];
+    if (r.pos < 0 || r.lo > r.pos) {
+      f_hi = -1;   // a row that sees nothing
+      continue;
+    }
+    const int64_t first = o.window > 0 ? std::max<int64_t>(r.lo, (int64_t)r.pos - o.window + 1)
+                                       : r.lo;
+    const int64_t sinks = std::min<int64_t>(first, (int64_t)r.lo + o.n_sinks);
+    w_lo = std::min(w_lo, first);
+    w_hi = std::max<int64_t>(w_hi, r.pos + 1);
+    if (sinks > r.lo) {
+      s_lo = std::min<int64_t>(s_lo, r.lo);
+      s_hi = std::max(s_hi, sinks);
+    }
+    f_lo = std::max(f_lo, first);
+    f_hi = std::min<int64_t>(f_hi, r.pos);
+  }
+  auto down = [](int64_t k) { return (int32_t)(k / kStepKeys); };
+  auto up = [](int64_t k) { return (int32_t)((k + kStepKeys - 1) / kStepKeys); };
+  it->a0 = it->a1 = it->b0 = it->b1 = 0;
+  if (w_lo < w_hi) {
+    it->b0 = down(w_lo);
+    it->b1 = up(w_hi);
+  }
+  if (s_lo < s_hi) {
+    it->a0 = down(s_lo);
+    it->a1 = up(s_hi);
+    if (it->a1 >= it->b0) {   // the ranges meet: one range
+      it->b0 = std::min(it->a0, it->b0);
+      it->b1 = std::max(it->a1, it->b1);
+      it->a0 = it->a1 = 0;
+    }
+  }
+  it->full_lo = (int32_t)std::min<int64_t>(f_lo, kNone);
+  it->full_hi = (int32_t)std::min<int64_t>(f_hi, kNone);
+}
+
+int32_t n_tiles(const StepItem& it) { return it.a1 - it.a0 + it.b1 - it.b0; }
+
+// The item's tiles [t0, t1), counted over its two ranges.
+StepItem cut(const StepItem& it, int32_t t0, int32_t t1) {
+  StepItem c = it;
+  const int32_t na = it.a1 - it.a0;
+  c.a0 = it.a0 + std::min(t0, na);
+  c.a1 = it.a0 + std::min(t1, na);
+  c.b0 = it.b0 + std::max(t0 - na, 0);
+  c.b1 = it.b0 + std::max(t1 - na, 0);
+  return c;
+}
+
+tsr_status build_step(const tsr_model* model, const tsr_step_request* reqs, int32_t n_req,
+                      int32_t n_req_pages, const tsr_step_options* options, tsr_step* p) {
+  tsr_status st = check_step_model(model);
+  if (st != TSR_OK) return st;
+  const tsr_model& m = *model;
+  tsr_step_options o{};
+  if (options) o = *options;
+  for (int32_t r : o.reserved)
+    if (r != 0) return fail(TSR_ERR_INVALID_ARG, "tsr_step_options.reserved must be zero");
+  if (o.window < 0 || o.n_sinks < 0)
+    return fail(TSR_ERR_INVALID_ARG, "tsr_step_options: window and n_sinks must be >= 0");
+  if (o.split_tiles < -1)
+    return fail(TSR_ERR_INVALID_ARG, "tsr_step_options.split_tiles must be -1, 0 or positive");
+  if (o.attn_kernel < 0 || o.attn_kernel > 2)
+    return fail(TSR_ERR_INVALID_ARG, "tsr_step_options.attn_kernel must be 0, 1 or 2");
+  if (n_req < 0 || (n_req > 0 && !reqs))
+    return fail(TSR_ERR_INVALID_ARG, "n_req < 0, or reqs is NULL");
+  if (n_req_pages < 0) return fail(TSR_ERR_INVALID_ARG, "n_req_pages must be >= 0");
+  if ((int64_t)n_req_pages * m.page_size >= INT32_MAX)
+    return fail(TSR_ERR_OUT_OF_RANGE, "arena too large: pages * page_size must fit int32");
+  // positions end below max_position: nothing is lost by these bounds
+  o.window = std::min(o.window, m.max_position);
+  o.n_sinks = o.window > 0 ? std::min(o.n_sinks, m.max_position) : 0;
+
+  p->model = m;
+  p->opt = o;
+  p->scale = m.softmax_scale > 0.0f ? m.softmax_scale
+                                    : (float)(1.0 / std::sqrt((double)m.head_dim));
+  p->n_req_pages = n_req_pages;
+  const int B = m.page_size, Hkv = m.n_kv_heads, G = m.n_q_heads / Hkv;
+
+  std::vector<StepRow> rows;
+  std::vector<int32_t> bts;
+  std::vector<StepPage> pages;
+  // per page: slots listed so far (page list), and whether a second entry of
+  // some block table names it
+  std::vector<int32_t> page_n((size_t)n_req_pages, 0);
+  std::vector<uint8_t> page_twice((size_t)n_req_pages, 0);
+  std::vector<int32_t> row0(n_req + 1, 0), bt_off(n_req, 0);
+  for (int r = 0; r < n_req; ++r) {
+    const tsr_step_request& q = reqs[r];
+    if (q.kv_len < 0 || q.n_rows < 0)
+      return fail_req(TSR_ERR_INVALID_ARG, r, "kv_len and n_rows must be >= 0");
+    if (q.kv_len > m.max_position)
+      return fail_req(TSR_ERR_OUT_OF_RANGE, r, "kv_len " + std::to_string(q.kv_len) +
+                                                   " exceeds max_position " +
+                                                   std::to_string(m.max_position));
+    if (q.kv_len > 0 && !q.block_table)
+      return fail_req(TSR_ERR_INVALID_ARG, r, "block_table is NULL");
+    if (!q.positions && q.n_rows > q.kv_len)
+      return fail_req(TSR_ERR_INVALID_ARG, r, "more rows than keys");
+    const int np = (q.kv_len + B - 1) / B;
+    bt_off[r] = (int32_t)bts.size();
+    if (bts.size() + np > INT32_MAX / 2)
+      return fail(TSR_ERR_OUT_OF_RANGE, "block tables too large");
+    for (int i = 0; i < np; ++i) {
+      const int32_t pg = q.block_table[i];
+      if (pg < 0 || pg >= n_req_pages)
+        return fail_req(TSR_ERR_OUT_OF_RANGE, r, "block_table[" + std::to_string(i) + "] = " +
+                                                     std::to_string(pg) +
+                                                     " is outside the request arena");
+      bts.push_back(pg);
+      if (page_n[pg]) page_twice[pg] = 1;
+      page_n[pg] = std::max(page_n[pg], std::min(B, q.kv_len - i * B));
+    }
+    int32_t prev = -1;
+    for (int i = 0; i < q.n_rows; ++i) {
+      StepRow row{-1, 0, -1, 0};
+      const int32_t pos = q.positions ? q.positions[i] : q.kv_len - q.n_rows + i;
+      if (pos < -1 || pos >= q.kv_len)
+        return fail_req(TSR_ERR_OUT_OF_RANGE, r, "position " + std::to_string(pos) +
+                                                     " is outside [-1, kv_len)");
+      if (pos >= 0) {
+        if (pos <= prev)
+          return fail_req(TSR_ERR_INVALID_ARG, r, "positions must ascend");
+        prev = pos;
+        row.pos = pos;
+        row.lo = q.row_lo ? q.row_lo[i] : 0;
+        if (row.lo < 0 || row.lo > pos + 1)
+          return fail_req(TSR_ERR_OUT_OF_RANGE, r, "row_lo " + std::to_string(row.lo) +
+                                                       " is outside [0, position + 1]");
+        row.dst = q.block_table[pos / B] * B + pos % B;
+      }
+      rows.push_back(row);
+    }
+    if (rows.size() > (size_t)INT32_MAX / 64 / 256)
+      return fail(TSR_ERR_OUT_OF_RANGE, "too many rows");
+    row0[r + 1] = (int32_t)rows.size();
+  }
+  p->T = (int32_t)rows.size();
+  p->shared_append = false;
+  for (const StepRow& r : rows)
+    if (r.pos >= 0 && page_twice[r.dst / B]) p->shared_append = true;
+  for (int32_t i = 0; i < n_req_pages; ++i)
+    if (page_n[i]) pages.push_back({i, page_n[i]});
+
+  // attention items: row tile x head block x KV head
+  p->item_vecs = kStepVecs;
+  const int hb = std::min(G, kStepVecs);              // heads of an item
+  const int rt = std::max(1, kStepVecs / hb);         // rows of an item
+  std::vector<StepItem> whole;
+  for (int r = 0; r < n_req; ++r)
+    for (int i = row0[r]; i < row0[r + 1]; i += rt) {
+      StepItem it{};
+      it.row0 = i;
+      it.n_rows = std::min(rt, row0[r + 1] - i);
+      it.bt_off = bt_off[r];
+      it.kv_len = reqs[r].kv_len;
+      it.part_slot = -1;
+      item_keys(rows, i, it.n_rows, o, &it);
+      for (int g = 0; g < Hkv; ++g)
+        for (int h = 0; h < G; h += hb) {
+          it.kv_head = g;
+          it.head0 = h;
+          it.n_heads = std::min(hb, G - h);
+          whole.push_back(it);
+        }
+    }
+  if (whole.size() > (size_t)INT32_MAX / 4)
+    return fail(TSR_ERR_OUT_OF_RANGE, "too many attention items");
+
+  // key ranges
+  int64_t total = 0;
+  for (const StepItem& it : whole) total += n_tiles(it);
+  int64_t cap = INT32_MAX;
+  if (o.split_tiles > 0) cap = o.split_tiles;
+  if (o.split_tiles == 0) {
+    const int64_t want = (int64_t)kRangesPerCu * kNumCus;
+    cap = std::max<int64_t>(kMinRangeTiles, (total + want - 1) / want);
+  }
+  std::vector<StepItem> items;
+  std::vector<StepMerge> merges;
+  int64_t slots = 0;
+  for (const StepItem& it : whole) {
+    const int64_t n = n_tiles(it);
+    int64_t parts = std::max<int64_t>(1, (n + cap - 1) / cap);
+    if (parts > 1 && slots + parts > kMaxStepSlots) {
+      if (o.split_tiles > 0)
+        return fail(TSR_ERR_OUT_OF_RANGE, "split_tiles cuts this step into too many ranges");
+      parts = 1;
+    }
+    if (parts == 1) {
+      items.push_back(it);
+      continue;
+    }
+    StepMerge mg{};
+    mg.row0 = it.row0;
+    mg.n_rows = it.n_rows;
+    mg.hq0 = it.kv_head * G + it.head0;
+    mg.n_heads = it.n_heads;
+    mg.slot0 = (int32_t)slots;
+    mg.n_slots = (int32_t)parts;
+    merges.push_back(mg);
+    for (int64_t c = 0; c < parts; ++c) {
+      StepItem x = cut(it, (int32_t)(n * c / parts), (int32_t)(n * (c + 1) / parts));
+      x.part_slot = (int32_t)slots++;
+      items.push_back(x);
+    }
+  }
+  // longest first: the launch ends with its short items
+  std::stable_sort(items.begin(), items.end(), [](const StepItem& a, const StepItem& b) {
+    return n_tiles(a) > n_tiles(b);
+  });
+  p->n_items = (int32_t)items.size();
+  p->n_merges = (int32_t)merges.size();
+  p->n_pages = (int32_t)pages.size();
+
+  size_t off = 0;
+  auto place = [&](size_t bytes) {
+    const size_t at = off;
+    off = align_up(off + bytes, 256);
+    return at;
+  };
+  p->off_rows = place(rows.size() * sizeof(StepRow));
+  p->off_items = place(items.size() * sizeof(StepItem));
+  p->off_merges = place(merges.size() * sizeof(StepMerge));
+  p->off_pages = place(pages.size() * sizeof(StepPage));
+  p->off_bts = place(bts.size() * sizeof(int32_t));
+  p->image_bytes = std::max<size_t>(off, 256);
+  // the split buffer is written by the kernels, not uploaded
+  p->off_split_o = place((size_t)slots * p->item_vecs * m.head_dim * sizeof(float));
+  p->off_split_lse = place((size_t)slots * p->item_vecs * sizeof(float));
+  p->ws_bytes = std::max<size_t>(off, 256);
+  p->image.assign(p->image_bytes, 0);
+  auto put = [&](size_t at, const void* src, size_t bytes) {
+    if (bytes) std::memcpy(p->image.data() + at, src, bytes);
+  };
+  put(p->off_rows, rows.data(), rows.size() * sizeof(StepRow));
+  put(p->off_items, items.data(), items.size() * sizeof(StepItem));
+  put(p->off_merges, merges.data(), merges.size() * sizeof(StepMerge));
+  put(p->off_pages, pages.data(), pages.size() * sizeof(StepPage));
+  put(p->off_bts, bts.data(), bts.size() * sizeof(int32_t));
+  return TSR_OK;
+}
+
+tsr_status check_exec(const tsr_step* p) {
+  if (!p) return fail(TSR_ERR_INVALID_ARG, "step is NULL");
+  if (!p->ws)
+    return fail(TSR_ERR_INVALID_ARG,
+                "step was created without a device workspace (host-only step)");
+  return TSR_OK;
+}
+
+bool is_e2m1(const tsr_step* p) { return p->model.kv_dtype == TSR_E2M1; }
+
+tsr_status check_scale(const tsr_step* p, const void* scale) {
+  if (is_e2m1(p) == (scale != nullptr)) return TSR_OK;
+  return fail(TSR_ERR_INVALID_ARG, is_e2m1(p) ? "4-bit pages need their scale array"
+                                              : "req_scale applies to 4-bit pages only; pass NULL");
+}
+
+bool aligned(std::initializer_list<const void*> ptrs) {
+  for (const void* x : ptrs)
+    if (reinterpret_cast<uintptr_t>(x) % 16) return false;
+  return true;
+}
+
+tsr_status misaligned() {
+  return fail(TSR_ERR_INVALID_ARG, "a pointer is not 16-byte aligned");
+}
+
+tsr_status null_pointer(const char* what) {
+  return fail(TSR_ERR_INVALID_ARG, std::string(what) + ": a required pointer is NULL");
+}
+
+}  // namespace
+
+tsr_status check_step_model(const tsr_model* m) {
+  tsr_status st = check_model_fields(m);
+  if (st != TSR_OK) return st;
+  if (m->n_q_heads / m->n_kv_heads > 64)
+    return fail(TSR_ERR_UNSUPPORTED, "steps support at most 64 query heads per KV head");
+  if (m->n_q_heads > 4096)
+    return fail(TSR_ERR_UNSUPPORTED, "steps support at most 4096 query heads");
+  if (m->kv_dtype == TSR_F32 && m->act_dtype == TSR_F32) {
+    if (m->head_dim != 64 && m->head_dim != 128 && m->head_dim != 256)
+      return fail(TSR_ERR_UNSUPPORTED, "fp32 steps support head_dim 64, 128, 256");
+    return TSR_OK;
+  }
+  if ((m->kv_dtype == TSR_BF16 || m->kv_dtype == TSR_E2M1) && m->act_dtype == TSR_BF16) {
+    if (m->head_dim != 128)
+      return fail(TSR_ERR_UNSUPPORTED, "bf16 and 4-bit steps support head_dim 128");
+    if (m->page_size < 16)
+      return fail(TSR_ERR_UNSUPPORTED, "bf16 and 4-bit steps need page_size >= 16");
+    return TSR_OK;
+  }
+  return fail(TSR_ERR_UNSUPPORTED, "steps support (kv, act) dtypes (F32, F32), (BF16, BF16) and "
+                                   "(E2M1, BF16)");
+}
+
+}  // namespace tsr
+
+using namespace tsr;
+
+extern "C" {
+
+size_t tsr_step_workspace_size(const tsr_model* model, const tsr_step_request* reqs,
+                               int32_t n_req, int32_t n_req_pages,
+                               const tsr_step_options* options) {
+  size_t bytes = 0;
+  guarded([&]() -> tsr_status {
+    tsr_step tmp{};
+    tsr_status st = build_step(model, reqs, n_req, n_req_pages, options, &tmp);
+    if (st == TSR_OK) bytes = tmp.ws_bytes;
+    return st;
+  });
+  return bytes;
+}
+
+tsr_status tsr_step_create(const tsr_model* model, const tsr_step_request* reqs, int32_t n_req,
+                           int32_t n_req_pages, const tsr_step_options* options,
+                           const void* dev_rope_table, void* dev_workspace,
+                           size_t workspace_bytes, void* stream, tsr_step** out_step) {
+  return guarded([&]() -> tsr_status {
+    if (!out_step) return fail(TSR_ERR_INVALID_ARG, "out_step is NULL");
+    *out_step = nullptr;
+    std::unique_ptr<tsr_step> p(new tsr_step());
+    tsr_status st = build_step(model, reqs, n_req, n_req_pages, options, p.get());
+    if (st != TSR_OK) return st;
+    if (dev_workspace) {
+      if (workspace_bytes < p->ws_bytes)
+        return fail(TSR_ERR_INVALID_ARG, "workspace smaller than tsr_step_workspace_size() = " +
+                                             std::to_string(p->ws_bytes));
+      if (!dev_rope_table) return fail(TSR_ERR_INVALID_ARG, "dev_rope_table is NULL");
+      if (reinterpret_cast<uintptr_t>(dev_workspace) % 256 || !aligned({dev_rope_table}))
+        return fail(TSR_ERR_INVALID_ARG, "dev_workspace must be 256-byte and dev_rope_table "
+                                         "16-byte aligned");
+      hipError_t e = hipMemcpyAsync(dev_workspace, p->image.data(), p->image_bytes,
+                                    hipMemcpyHostToDevice, static_cast<hipStream_t>(stream));
+      if (e != hipSuccess) return device_fail("hipMemcpyAsync(step)", e);
+      char* base = static_cast<char*>(dev_workspace);
+      const size_t half = (size_t)p->model.max_position * (p->model.head_dim / 2);
+      p->dev.rows = reinterpret_cast<const StepRow*>(base + p->off_rows);
+      p->dev.items = reinterpret_cast<const StepItem*>(base + p->off_items);
+      p->dev.merges = reinterpret_cast<const StepMerge*>(base + p->off_merges);
+      p->dev.pages = reinterpret_cast<const StepPage*>(base + p->off_pages);
+      p->dev.bts = reinterpret_cast<const int32_t*>(base + p->off_bts);
+      p->dev.split_o = reinterpret_cast<float*>(base + p->off_split_o);
+      p->dev.split_lse = reinterpret_cast<float*>(base + p->off_split_lse);
+      p->dev.rope_cos = static_cast<const float*>(dev_rope_table);
+      p->dev.rope_sin = p->dev.rope_cos + half;
+      p->ws = dev_workspace;
+    }
+    *out_step = p.release();
+    return TSR_OK;
+  });
+}
+
+void tsr_step_destroy(tsr_step* p) { delete p; }
+
+int32_t tsr_step_num_rows(const tsr_step* p) { return p ? p->T : -1; }
+int32_t tsr_step_num_attn_items(const tsr_step* p) { return p ? p->n_items : -1; }
+int32_t tsr_step_num_attn_splits(const tsr_step* p) { return p ? p->n_merges : -1; }
+int32_t tsr_step_attn_item_rows(const tsr_step* p) { return p ? p->item_vecs : -1; }
+
+tsr_status tsr_step_append(const tsr_step* p, const tsr_qk_norm* norm, const void* q,
+                           int64_t q_stride, const void* k, int64_t k_stride, const void* v,
+                           int64_t v_stride, void* q_out, void* k_pre, void* req_k, void* req_v,
+                           void* req_scale, void* stream) {
+  return guarded([&]() -> tsr_status {
+    tsr_status st = check_exec(p);
+    if (st != TSR_OK) return st;
+    if ((st = check_scale(p, req_scale)) != TSR_OK) return st;
+    const tsr_model& m = p->model;
+    if (norm) {
+      if (norm->reserved != 0) return fail(TSR_ERR_INVALID_ARG, "tsr_qk_norm.reserved must be 0");
+      if (!(norm->eps > 0.0f) || !std::isfinite(norm->eps))
+        return fail(TSR_ERR_INVALID_ARG, "tsr_qk_norm.eps must be positive and finite");
+      if (!aligned({norm->q_weight, norm->k_weight})) return misaligned();
+    }
+    if (p->shared_append)
+      return fail(TSR_ERR_INVALID_ARG, "a page the step's rows are appended to is in a block "
+                                       "table twice");
+    const int64_t packed_q = (int64_t)m.n_q_heads * m.head_dim;
+    const int64_t packed_kv = (int64_t)m.n_kv_heads * m.head_dim;
+    const int per16 = m.act_dtype == TSR_F32 ? 4 : 8;
+    int64_t* strides[3] = {&q_stride, &k_stride, &v_stride};
+    for (int i = 0; i < 3; ++i) {
+      const int64_t least = i == 0 ? packed_q : packed_kv;
+      if (*strides[i] == 0) *strides[i] = least;
+      if (*strides[i] < least || *strides[i] > ((int64_t)1 << 40) || *strides[i] % per16)
+        return fail(TSR_ERR_INVALID_ARG, "row strides must hold a row and be multiples of 16 "
+                                         "bytes");
+    }
+    if (p->T == 0) return TSR_OK;
+    if (!q || !k || !v || !q_out || !req_k || !req_v) return null_pointer("step_append");
+    if (!aligned({q, k, v, q_out, k_pre, req_k, req_v, req_scale})) return misaligned();
+    if ((q_out == q && q_stride != packed_q) || (k_pre == k && k_stride != packed_kv))
+      return fail(TSR_ERR_INVALID_ARG, "q_out and k_pre may be q and k only if those are packed");
+    hipError_t e = launch_step_append(p, norm, q, q_stride, k, k_stride, v, v_stride, q_out,
+                                      k_pre, req_k, req_v, req_scale,
+                                      static_cast<hipStream_t>(stream));
+    if (e != hipSuccess) return device_fail("step append launch", e);
+    return TSR_OK;
+  });
+}
+
+tsr_status tsr_step_attn(const tsr_step* p, const void* q, const void* req_k,
+                         const void* req_v, const void* req_scale, void* out, float* lse,
+                         void* stream) {
+  return guarded([&]() -> tsr_status {
+    tsr_status st = check_exec(p);
+    if (st != TSR_OK) return st;
+    if ((st = check_scale(p, req_scale)) != TSR_OK) return st;
+    if (p->T == 0) return TSR_OK;
+    if (!q || !req_k || !req_v || !out) return null_pointer("step_attn");
+    if (!aligned({q, req_k, req_v, req_scale, out, lse})) return misaligned();
+    hipError_t e = launch_step_attn(p, q, req_k, req_v, req_scale, out, lse,
+                                    static_cast<hipStream_t>(stream));
+    if (e != hipSuccess) return device_fail("step attention launch", e);
+    return TSR_OK;
+  });
+}
+
+tsr_status tsr_step_pack_kv(const tsr_step* p, const void* bf16_k, const void* bf16_v,
+                            void* req_k, void* req_v, void* req_scale, void* stream) {
+  return guarded([&]() -> tsr_status {
+    tsr_status st = check_exec(p);
+    if (st != TSR_OK) return st;
+    if (!is_e2m1(p))
+      return fail(TSR_ERR_INVALID_ARG, "pack_kv applies to steps of a 4-bit (E2M1) model");
+    if (p->n_pages == 0) return TSR_OK;
+    if (!bf16_k || !bf16_v || !req_k || !req_v || !req_scale) return null_pointer("step_pack_kv");
+    if (!aligned({bf16_k, bf16_v, req_k, req_v, req_scale})) return misaligned();
+    hipError_t e = launch_step_pack(p, bf16_k, bf16_v, req_k, req_v, req_scale,
+                                    static_cast<hipStream_t>(stream));
+    if (e != hipSuccess) return device_fail("step pack launch", e);
+    return TSR_OK;
+  });
+}
+
+tsr_status tsr_step_unpack_kv(const tsr_step* p, const void* req_k, const void* req_v,
+                              const void* req_scale, void* bf16_k, void* bf16_v, void* stream) {
+  return guarded([&]() -> tsr_status {
+    tsr_status st = check_exec(p);
+    if (st != TSR_OK) return st;
+    if (!is_e2m1(p))
+      return fail(TSR_ERR_INVALID_ARG, "unpack_kv applies to steps of a 4-bit (E2M1) model");
+    if (p->n_pages == 0) return TSR_OK;
+    if (!bf16_k || !bf16_v || !req_k || !req_v || !req_scale)
+      return null_pointer("step_unpack_kv");
+    if (!aligned({bf16_k, bf16_v, req_k, req_v, req_scale})) return misaligned();
+    hipError_t e = launch_step_unpack(p, req_k, req_v, req_scale, bf16_k, bf16_v,
+                                      static_cast<hipStream_t>(stream));
+    if (e != hipSuccess) return device_fail("step unpack launch", e);
+    return TSR_OK;
+  });
+}
+
+}  // extern "C"

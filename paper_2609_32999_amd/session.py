@@ -9,9 +9,13 @@ in libtsr's kernels through the C ABI.  A Session owns, for one layer shape:
 * the request arena  [n_req_pages][H_kv][B][d] for the assembled K and V;
 * the RoPE table     built once per model by tsr_rope_table_init;
 * for e4m3 pools, page scales [n_layers][pages][2] fp32 ({K, V}) for both
-  arenas.
+  arenas;
+* with four_bit=True, a second request arena under the same page ids that
+  holds the pages in 4 bits: codes [n_req_pages][H_kv][B][d/2] for K and V and
+  scales [n_req_pages][2][H_kv][B][d/32].
 
-Plans (one per batch of requests) own their device workspace.
+Plans (one per batch of requests) and steps (one per pass over request pages
+that are already there) own their device workspace.
 """
 from __future__ import annotations
 
@@ -43,10 +47,12 @@ def _host_device_pointer(t: torch.Tensor) -> int:
 
 class Session:
     def __init__(self, shape, n_pool_pages: int, n_req_pages: int,
-                 device: str = "cuda", n_layers: int = 1, stream=None, pool: str = "device"):
+                 device: str = "cuda", n_layers: int = 1, stream=None, pool: str = "device",
+                 four_bit: bool = False):
         """`shape` has n_q_heads, n_kv_heads, head_dim, page_size, kv_dtype,
         act_dtype, rope_theta, max_position (workloads.ModelShape).  `pool`
-        is "device" (HBM) or "host" (pinned host memory: the host tier)."""
+        is "device" (HBM) or "host" (pinned host memory: the host tier);
+        `four_bit` adds a 4-bit request arena (bf16 shapes)."""
         _require_device()
         B.lib()
         self.shape = shape
@@ -84,6 +90,20 @@ class Session:
                                           **pool_dev)
             self.req_scale = torch.empty((n_layers, n_req_pages, 2), dtype=torch.float32,
                                          device=self.device)
+        self.req4_k = self.req4_v = self.req4_scale = None
+        if four_bit:
+            if shape.kv_dtype != "bf16":
+                raise B.TsrError(B.TSR_ERR_UNSUPPORTED, "four_bit needs a bf16 shape")
+            codes = (*page[:2], shape.head_dim // 2)
+            self.model4 = B.make_model(shape.n_q_heads, shape.n_kv_heads, shape.head_dim,
+                                       shape.page_size, "e2m1", shape.act_dtype,
+                                       shape.rope_theta, shape.max_position)
+            self.req4_k = torch.empty((n_layers, n_req_pages, *codes), dtype=torch.uint8,
+                                      device=self.device)
+            self.req4_v = torch.empty_like(self.req4_k)
+            self.req4_scale = torch.empty((n_layers, n_req_pages, 2, *page[:2],
+                                           shape.head_dim // 32), dtype=torch.uint8,
+                                          device=self.device)
         # addresses the kernels use for the pool arenas
         self._pool_base = {}
         kv_base = (self.pool_kv.data_ptr() if pool == "device"
@@ -210,3 +230,89 @@ class Session:
     def retain(self, plan, k, v, layer: int = 0, stream=None):
         B.tsr_retain_kv(plan, k, v, self._pk(layer), self._pv(layer), self._ps(layer),
                         stream or self.stream)
+
+    # ------------------------------------- steps over request pages in place
+    def step(self, requests, stream=None, four_bit: bool = False, window: int = 0,
+             n_sinks: int = 0, split_tiles: int = 0, attn_kernel: int = 0):
+        """Validate and upload a step: rows of requests whose KV is in request
+        pages (objects with kv_len, n_rows, block_table, and optionally
+        positions and row_lo).  `four_bit`: over the 4-bit arena.  `window`
+        and `n_sinks` are its attention's sliding window and sinks."""
+        if four_bit and self.req4_k is None:
+            raise ValueError("the session was made without four_bit=True")
+        model = self.model4 if four_bit else self.model
+        batch = B.StepBatch(requests)
+        opts = dict(window=window, n_sinks=n_sinks, split_tiles=split_tiles,
+                    attn_kernel=attn_kernel)
+        n = B.tsr_step_workspace_size(model, batch, self.n_req_pages, **opts)
+        ws = torch.empty(n, dtype=torch.uint8, device=self.device)
+        step = B.tsr_step_create(model, batch, self.n_req_pages, self.rope, ws, n,
+                                 stream or self.stream, **opts)
+        step.workspace = ws     # keep the workspace alive with the step
+        step.batch = batch
+        step.four_bit = four_bit
+        return step
+
+    def _step_kv(self, step, layer):
+        if step.four_bit:
+            return self.req4_k[layer], self.req4_v[layer], self.req4_scale[layer]
+        return self.req_k[layer], self.req_v[layer], None
+
+    def _rows(self, step, x, heads, what):
+        """A [rows][heads][d] tensor of the activation type with rows any
+        distance apart; returns that distance in elements."""
+        d = self.shape.head_dim
+        if (x.dtype != self.act_dtype or tuple(x.shape) != (step.num_rows, heads, d) or
+                x.device != self.req_k.device):
+            raise ValueError(f"{what} must be a [{step.num_rows}][{heads}][{d}] tensor of "
+                             f"{self.act_dtype} on {self.req_k.device}")
+        if step.num_rows and (x.stride(2) != 1 or (heads > 1 and x.stride(1) != d)):
+            raise ValueError(f"{what}: the heads of a row must be contiguous")
+        return x.stride(0) if step.num_rows > 1 else 0
+
+    def step_append(self, step, q, k, v, q_out, k_pre=None, q_weight=None, k_weight=None,
+                    eps: float | None = None, layer: int = 0, stream=None):
+        """Norms (if `eps` is given), RoPE and the page write of a step's rows.
+        q, k and v may be views of one projection's output."""
+        h, g = self.shape.n_q_heads, self.shape.n_kv_heads
+        strides = (self._rows(step, q, h, "q"), self._rows(step, k, g, "k"),
+                   self._rows(step, v, g, "v"))
+        for x, n, what in ((q_out, h, "q_out"), (k_pre, g, "k_pre")):
+            if x is not None:
+                self._rows(step, x, n, what)
+                if not x.is_contiguous():
+                    raise ValueError(f"{what} must be contiguous")
+        for w in (q_weight, k_weight):
+            if w is not None and (eps is None or w.dtype != self.act_dtype or
+                                  tuple(w.shape) != (self.shape.head_dim,) or
+                                  not w.is_contiguous() or w.device != self.req_k.device):
+                raise ValueError("norm weights are [head_dim] of the activation type on the "
+                                 "session's device, and need eps")
+        norm = None if eps is None else B.make_qk_norm(q_weight, k_weight, eps)
+        rk, rv, rs = self._step_kv(step, layer)
+        B.tsr_step_append(step, q, k, v, rk, rv, rs, q_out, k_pre, norm, *strides,
+                          stream=stream or self.stream)
+
+    def step_attn(self, step, q, out, lse=None, layer: int = 0, stream=None):
+        """Attention of a step's rows; q is step_append's q_out."""
+        for x, what in ((q, "q"), (out, "out")):
+            self._rows(step, x, self.shape.n_q_heads, what)
+            if not x.is_contiguous():
+                raise ValueError(f"{what} must be contiguous")
+        if lse is not None and (lse.dtype != torch.float32 or not lse.is_contiguous() or
+                                tuple(lse.shape) != (step.num_rows, self.shape.n_q_heads) or
+                                lse.device != self.req_k.device):
+            raise ValueError("lse must be a contiguous fp32 [rows][n_q_heads] tensor")
+        rk, rv, rs = self._step_kv(step, layer)
+        B.tsr_step_attn(step, q, rk, rv, rs, out, lse, stream or self.stream)
+
+    def pack_step(self, step, layer: int = 0, stream=None):
+        """bf16 request pages of a four_bit step's requests -> 4-bit pages."""
+        B.tsr_step_pack_kv(step, self.req_k[layer], self.req_v[layer], self.req4_k[layer],
+                           self.req4_v[layer], self.req4_scale[layer], stream or self.stream)
+
+    def unpack_step(self, step, layer: int = 0, stream=None):
+        """4-bit request pages of a four_bit step's requests -> bf16 pages."""
+        B.tsr_step_unpack_kv(step, self.req4_k[layer], self.req4_v[layer],
+                             self.req4_scale[layer], self.req_k[layer], self.req_v[layer],
+                             stream or self.stream)

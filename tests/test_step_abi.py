@@ -1,0 +1,185 @@
+"""Steps over request pages on the host: what they refuse, and how they cut
+their attention.  No GPU."""
+from types import SimpleNamespace as NS
+
+import numpy as np
+import pytest
+
+import paper_2609_32999_amd as P
+import workloads
+from paper_2609_32999_amd import _binding as B
+
+
+def model(hq=8, hkv=2, d=128, page=16, kv="bf16", act=None, **kw):
+    return P.make_model(hq, hkv, d, page, kv, act or ("f32" if kv == "f32" else "bf16"), **kw)
+
+
+def req(kv_len=40, n_rows=1, page=16, first=0, positions=None, row_lo=None, table=None):
+    n = -(-kv_len // page)
+    return NS(kv_len=kv_len, n_rows=n_rows, positions=positions, row_lo=row_lo,
+              block_table=list(range(first, first + n)) if table is None else table)
+
+
+def make(reqs, m=None, pages=64, **kw):
+    return P.tsr_step_create(m or model(), P.StepBatch(reqs), pages, **kw)
+
+
+def refused(status, match, reqs=None, m=None, pages=64, **kw):
+    reqs = [req()] if reqs is None else reqs
+    with pytest.raises(P.TsrError, match=match or None) as e:
+        make(reqs, m, pages, **kw)
+    assert e.value.status == status
+    with pytest.raises(P.TsrError, match=match or None):
+        P.tsr_step_workspace_size(m or model(), P.StepBatch(reqs), pages, **kw)
+
+
+@pytest.mark.parametrize("kw", [dict(d=64), dict(d=256), dict(page=8), dict(kv="e4m3"),
+                                dict(kv="f32", d=96), dict(kv="e2m1", act="f32"),
+                                dict(kv="e2m1", page=8), dict(hq=130, hkv=2),
+                                dict(rope_interleaved=1)])
+def test_unsupported_models(kw):
+    refused(P.TSR_ERR_UNSUPPORTED, "", m=model(**kw))
+
+
+@pytest.mark.parametrize("kw", [dict(), dict(hq=10), dict(hq=128), dict(page=64), dict(kv="e2m1"),
+                                dict(kv="f32", d=64, page=8), dict(kv="f32", d=256)])
+def test_supported_models(kw):
+    m = model(**kw)
+    r = req(page=m.page_size)
+    assert make([r], m).num_rows == 1
+    n = P.tsr_step_workspace_size(m, P.StepBatch([r]), 64)
+    assert n > 0 and n % 256 == 0
+    assert P.tsr_rope_table_bytes(m) == 4 * m.max_position * m.head_dim
+
+
+def test_plans_refuse_four_bit_models():
+    wl = workloads.generate("small_bf16")
+    m = model(32, 8, kv="e2m1")
+    with pytest.raises(P.TsrError) as e:
+        P.tsr_plan_create(m, P.RequestBatch(wl.requests), wl.n_pool_pages, wl.n_req_pages)
+    assert e.value.status == P.TSR_ERR_UNSUPPORTED
+
+
+@pytest.mark.parametrize("status,match,reqs", [
+    (P.TSR_ERR_INVALID_ARG, "must be >= 0", [req(kv_len=-1, table=[0])]),
+    (P.TSR_ERR_INVALID_ARG, "must be >= 0", [req(n_rows=-1)]),
+    (P.TSR_ERR_INVALID_ARG, "more rows than keys", [req(kv_len=3, n_rows=4)]),
+    (P.TSR_ERR_OUT_OF_RANGE, "max_position", [req(kv_len=70000, table=[0])]),
+    (P.TSR_ERR_OUT_OF_RANGE, "outside the request arena", [req(table=[0, 64, 1])]),
+    (P.TSR_ERR_OUT_OF_RANGE, "outside the request arena", [req(table=[0, -1, 1])]),
+    (P.TSR_ERR_OUT_OF_RANGE, "position 40", [req(positions=[40])]),
+    (P.TSR_ERR_OUT_OF_RANGE, "position -2", [req(positions=[-2])]),
+    (P.TSR_ERR_INVALID_ARG, "ascend", [req(n_rows=2, positions=[5, 5])]),
+    (P.TSR_ERR_INVALID_ARG, "ascend", [req(n_rows=3, positions=[5, -1, 4])]),
+    (P.TSR_ERR_OUT_OF_RANGE, "row_lo 7", [req(positions=[5], row_lo=[7])]),
+    (P.TSR_ERR_OUT_OF_RANGE, "row_lo -1", [req(positions=[5], row_lo=[-1])]),
+    (P.TSR_ERR_OUT_OF_RANGE, "request 1", [req(), req(positions=[99], first=8)]),
+])
+def test_refused_requests(status, match, reqs):
+    refused(status, match, reqs)
+
+
+def test_null_block_table_and_arena_bounds():
+    r = req()
+    r.block_table = None
+    refused(P.TSR_ERR_INVALID_ARG, "block_table is NULL", [r])
+    refused(P.TSR_ERR_INVALID_ARG, "n_req_pages", pages=-1)
+    refused(P.TSR_ERR_OUT_OF_RANGE, "arena too large", pages=1 << 27)
+
+
+@pytest.mark.parametrize("kw", [dict(window=-1), dict(n_sinks=-1), dict(split_tiles=-2),
+                                dict(attn_kernel=3), dict(attn_kernel=-1)])
+def test_refused_options(kw):
+    refused(P.TSR_ERR_INVALID_ARG, "", **kw)
+
+
+def test_reserved_fields_are_refused():
+    o = B.tsr_step_options()
+    o.reserved[2] = 1
+    b = P.StepBatch([req()])
+    assert P.lib().tsr_step_workspace_size(B.ctypes.byref(model()), b.array, 1, 64,
+                                           B.ctypes.byref(o)) == 0
+    assert "reserved" in P.tsr_last_error()
+
+
+def test_batch_checks_row_counts():
+    with pytest.raises(ValueError, match="positions"):
+        P.StepBatch([req(n_rows=2, positions=[1])])
+
+
+def test_null_and_host_only_steps_do_not_run():
+    s = make([req()])
+    calls = [lambda: P.tsr_step_append(s, 16, 16, 16, 16, 16, None, 16),
+             lambda: P.tsr_step_attn(s, 16, 16, 16, None, 16),
+             lambda: P.tsr_step_pack_kv(s, 16, 16, 16, 16, 16),
+             lambda: P.tsr_step_unpack_kv(s, 16, 16, 16, 16, 16)]
+    for c in calls:
+        with pytest.raises(P.TsrError, match="host-only"):
+            c()
+    s.destroy()
+    assert s.handle is None
+    for c in calls:
+        with pytest.raises(P.TsrError, match="step is NULL"):
+            c()
+    assert P.lib().tsr_step_num_rows(None) == -1
+    assert P.lib().tsr_step_attn_item_rows(None) == -1
+
+
+def test_workspace_checks():
+    for kw, match in ((dict(dev_workspace=256, workspace_bytes=8), "workspace smaller"),
+                      (dict(dev_workspace=256, workspace_bytes=1 << 30), "dev_rope_table is NULL"),
+                      (dict(dev_workspace=264, workspace_bytes=1 << 30, dev_rope_table=256),
+                       "aligned")):
+        with pytest.raises(P.TsrError, match=match):
+            make([req()], **kw)
+
+
+def test_empty_and_padded_batches():
+    assert make([]).num_rows == 0
+    assert make([], pages=0).num_attn_items == 0
+    s = make([req(kv_len=0, n_rows=2, positions=[-1, -1], table=[]), req(n_rows=0)])
+    # two rows that hold no token: they still have outputs to clear
+    assert s.num_rows == 2 and s.num_attn_items > 0 and s.num_attn_splits == 0
+
+
+def test_few_row_items():
+    # 4 heads a group: 4 rows of a request share an item, per KV head
+    s = make([req(n_rows=9), req(n_rows=2, first=8)], split_tiles=-1, attn_kernel=1)
+    assert s.attn_item_rows == 16 and s.num_attn_items == 2 * (3 + 1)
+    # 5 heads: 3 rows; 20 heads: two head blocks a row
+    assert make([req(n_rows=9)], model(hq=10), split_tiles=-1, attn_kernel=1).num_attn_items == 2 * 3
+    assert make([req(n_rows=9)], model(hq=40), split_tiles=-1, attn_kernel=1).num_attn_items == 2 * 9 * 2
+
+
+def test_key_ranges():
+    long = [req(kv_len=16 * 1024, page=16)]
+    m = model(hq=8, hkv=2)
+    whole = make(long, m, 1024, split_tiles=-1)
+    assert whole.num_attn_items == 2 and whole.num_attn_splits == 0
+    cut = make(long, m, 1024, split_tiles=10)             # 512 tiles
+    assert cut.num_attn_items == 2 * 52 and cut.num_attn_splits == 2
+    auto = make(long, m, 1024)
+    assert auto.num_attn_splits == 2 and auto.num_attn_items > 16
+    # a window of 100 keys and 5 sinks: 4 or 5 tiles and one
+    win = make(long, m, 1024, window=100, n_sinks=5, split_tiles=1)
+    assert win.num_attn_items == 2 * (4 + 1) and win.num_attn_splits == 2
+    assert (P.tsr_step_workspace_size(m, P.StepBatch(long), 1024, split_tiles=10) >
+            P.tsr_step_workspace_size(m, P.StepBatch(long), 1024, split_tiles=-1))
+    refused(P.TSR_ERR_OUT_OF_RANGE, "too many ranges",
+            [req(kv_len=1 << 20, first=0) for _ in range(4)], model(max_position=1 << 20),
+            1 << 16, split_tiles=1)
+
+
+def test_step_of_a_plan_row_set():
+    """The rows of a composed prompt, with their first visible keys."""
+    cfg = workloads.get_config("small_bf16").with_(miss_scope="local")
+    wl = workloads.make_workload(cfg)
+    m = model(32, 8, max_position=wl.model.max_position)
+    plan = P.tsr_plan_create(m, P.RequestBatch(wl.requests), wl.n_pool_pages, wl.n_req_pages)
+    pos, r = plan.compute_positions()
+    lo = plan.row_kv_lo()
+    reqs = [NS(kv_len=q.prompt_len, n_rows=int((r == i).sum()), positions=pos[r == i],
+               row_lo=lo[r == i], block_table=q.block_table)
+            for i, q in enumerate(wl.requests)]
+    assert make(reqs, m, wl.n_req_pages).num_rows == plan.num_compute_tokens
+    assert np.any(lo > 0)
