@@ -130,8 +130,9 @@ tsr_status tsr_step_create(const tsr_model* model, const tsr_step_request* reqs,
                            size_t workspace_bytes, void* stream, tsr_step** out_step);
 void tsr_step_destroy(tsr_step* step);
 
-/* Rows T; attention work items; items whose key range was cut; rows an item
- * of the attention kernel holds, times query heads (16 or 128).  -1 for NULL. */
+/* Rows T; attention work items; items whose key range was cut; rows times
+ * query heads that the step's largest kind of item holds (16, or 256 where a
+ * request has rows for the second kernel of tsr_step_attn).  -1 for NULL. */
 int32_t tsr_step_num_rows(const tsr_step* step);
 int32_t tsr_step_num_attn_items(const tsr_step* step);
 int32_t tsr_step_num_attn_splits(const tsr_step* step);
@@ -169,7 +170,7 @@ tsr_status tsr_step_append(const tsr_step* step, const tsr_qk_norm* norm, const 
  * are fp32 (fp64 for fp32 models).
  * Two kernels for bf16 activations.  For few rows (16 rows x heads an item,
  * bound by reading the pages) the probabilities enter the second product as
- * two bf16 parts.  For many (128 an item, bound by the matrix cores) they and
+ * two bf16 parts.  For many (256 an item, bound by the matrix cores) they and
  * the values enter it as fp16: a value beyond 65504 in magnitude makes the
  * outputs that see it non-finite.  The second serves steps whose requests
  * have rows enough to fill its items. */

@@ -16,67 +16,11 @@
 #include "attn_common.h"
 #include "e2m1.h"
 #include "kernels_common.h"
-#include "step_internal.h"
+#include "step_device.h"
 
 namespace tsr {
 
 namespace {
-
-typedef float f32x4 __attribute__((ext_vector_type(4)));
-typedef short s16x4 __attribute__((ext_vector_type(4)));
-typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
-
-struct StepAttnArgs {
-  const StepRow* rows;
-  const StepItem* items;
-  const int32_t* bts;
-  const void *q, *k, *v;
-  const uint8_t* scales;
-  void* out;
-  float *lse, *split_o, *split_lse;
-  int32_t n_q_heads, n_kv_heads, log2_page, window, n_sinks;
-  float scale, scale_log2e;
-};
-
-// Keys a row sees: [wlo, pos] and [lo, shi); nothing if pos < 0.
-struct Sight {
-  int32_t lo, shi, wlo, pos;
-};
-__device__ __forceinline__ Sight row_sight(const StepRow& r, int window, int n_sinks) {
-  Sight s{r.lo, r.lo + n_sinks, r.lo, r.pos};
-  if (window > 0) s.wlo = max(r.lo, r.pos - window + 1);
-  return s;
-}
-__device__ __forceinline__ bool sees(const Sight& s, int key) {
-  return (key <= s.pos) & (key >= s.lo) & ((key >= s.wlo) | (key < s.shi));
-}
-
-// A uniform 32-bit load through the scalar cache.
-__device__ __forceinline__ int32_t uniform_i32(const int32_t* p) {
-  return *reinterpret_cast<const __attribute__((address_space(4))) int32_t*>(
-      reinterpret_cast<uintptr_t>(p));
-}
-
-template <int N>
-__device__ __forceinline__ void wait_vm() {
-  asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
-}
-__device__ __forceinline__ void wait_lds() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
-
-// Direct global->LDS loads, lane l's bytes at lds + 16 l (or 4 l): base
-// uniform, `off` the lane's byte offset.  The memory clobber keeps LDS reads
-// of the buffer on their side of it.
-#pragma clang diagnostic push
-#pragma clang diagnostic ignored "-Winline-asm"
-__device__ __forceinline__ void dma16(const void* base, uint32_t off, uint32_t lds) {
-  asm volatile("s_mov_b32 m0, %2\n\tglobal_load_lds_dwordx4 %0, %1"
-               :: "v"(off), "s"(base), "s"(lds) : "m0", "memory");
-}
-__device__ __forceinline__ void dma4(const void* base, uint32_t off, uint32_t lds) {
-  asm volatile("s_mov_b32 m0, %2\n\tglobal_load_lds_dword %0, %1"
-               :: "v"(off), "s"(base), "s"(lds) : "m0", "memory");
-}
-#pragma clang diagnostic pop
 
 // ------------------------------------------------ bf16 and 4-bit pages
 // A wave takes every fourth 32-key tile of the item's range and works alone
@@ -311,9 +255,7 @@ __global__ __launch_bounds__(64 * kStepWaves) void step_attn_kernel(const StepAt
     for (int db = 0; db < 8; ++db)
 #pragma unroll
       for (int b = 0; b < 2; ++b) {
-        const s16x4 x = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-            (lds_s16x4*)(uintptr_t)((va ^ (32 * db)) + 4096 * b));
-        const uint2 u = __builtin_bit_cast(uint2, x);
+        const uint2 u = lds_read_transposed((va ^ (32 * db)) + 4096 * b);
         vf[db].w[2 * b] = u.x;
         vf[db].w[2 * b + 1] = u.y;
       }
@@ -410,11 +352,11 @@ __global__ __launch_bounds__(64 * kStepWaves) void step_attn_kernel(const StepAt
     // nothing: 0, -inf
     const bool none = L == 0.0f;
     const float inv = none ? 0.0f : 1.0f / L;
-    float* po = a.split_o + ((int64_t)it.part_slot * kStepVecs + vec) * kD + d0;
+    float* po = a.split_o + ((int64_t)it.part_slot + vec) * kD + d0;
 #pragma unroll
     for (int e = 0; e < 8; ++e) acc[e] *= inv;
     store8(po, acc);
-    if (d0 == 0) a.split_lse[(int64_t)it.part_slot * kStepVecs + vec] = none ? -INFINITY : ls;
+    if (d0 == 0) a.split_lse[(int64_t)it.part_slot + vec] = none ? -INFINITY : ls;
     return;
   }
   const StepRow row = a.rows[it.row0 + r];
@@ -584,7 +526,7 @@ __global__ __launch_bounds__(64 * kStepWaves) void step_attn_f32_kernel(const St
       for (int x = 0; x < NW; ++x) sum += om[x][d][vec];
       const int64_t to = (int64_t)(it.row0 + r) * a.n_q_heads + it.kv_head * G + it.head0 + h;
       if (part)
-        a.split_o[((int64_t)it.part_slot * kStepVecs + vec) * D + 16 * t0 + d] = (float)sum;
+        a.split_o[((int64_t)it.part_slot + vec) * D + 16 * t0 + d] = (float)sum;
       else
         static_cast<float*>(a.out)[to * D + 16 * t0 + d] = (float)sum;
     }
@@ -592,7 +534,7 @@ __global__ __launch_bounds__(64 * kStepWaves) void step_attn_f32_kernel(const St
   if (w == 0 && c4 == 0 && real) {
     const float ls = zero ? -INFINITY : (float)(M + log(L));
     if (part)
-      a.split_lse[(int64_t)it.part_slot * kStepVecs + c16] = ls;
+      a.split_lse[(int64_t)it.part_slot + c16] = ls;
     else if (a.lse)
       a.lse[orow] = ls;
   }
@@ -619,10 +561,10 @@ __global__ __launch_bounds__(256) void step_merge_kernel(const MergeArgs a) {
   typedef float vec_t __attribute__((ext_vector_type(W)));
   const StepMerge g = a.merges[blockIdx.x];
   const int lane = threadIdx.x & 31;
-  const int vec = blockIdx.y * kMergeVecs + (threadIdx.x >> 5);
-  const int r = vec / g.n_heads, h = vec - r * g.n_heads;
+  const int v = blockIdx.y * kMergeVecs + (threadIdx.x >> 5);
+  const int r = (g.vec0 + v) / g.n_heads, h = g.vec0 + v - r * g.n_heads;
   if (r >= g.n_rows) return;
-  auto at = [&](int c) { return (int64_t)(g.slot0 + c) * kStepVecs + vec; };
+  auto at = [&](int c) { return (int64_t)g.slot0 + (int64_t)c * g.stride + v; };
   auto part = [&](int c) {
     return *reinterpret_cast<const vec_t*>(a.split_o + at(c) * D + W * lane);
   };
@@ -704,15 +646,22 @@ hipError_t launch_step_attn(const tsr_step* p, const void* q, const void* req_k,
   a.n_sinks = p->opt.n_sinks;
   a.scale = p->scale;
   a.scale_log2e = (float)((double)p->scale * 1.4426950408889634);
-  const dim3 grid(p->n_items), block(64 * kStepWaves);
+  const dim3 grid(p->n_items[0]), block(64 * kStepWaves);
   MergeArgs g{p->dev.rows, p->dev.merges, p->dev.split_o, p->dev.split_lse, out, lse,
               m.n_q_heads};
   const dim3 mgrid(p->n_merges, kStepVecs / kMergeVecs);
 #define TSR_STEP(KERNEL, E, D)                                               \
   do {                                                                       \
-    hipLaunchKernelGGL(KERNEL, grid, block, 0, s, a);                        \
+    if (grid.x > 0) hipLaunchKernelGGL(KERNEL, grid, block, 0, s, a);        \
     hipError_t e = hipGetLastError();                                        \
-    if (e != hipSuccess || p->n_merges == 0) return e;                       \
+    if (e != hipSuccess) return e;                                           \
+    if (p->n_items[1] > 0) {                                                 \
+      StepAttnArgs b = a;                                                    \
+      b.items += p->n_items[0];                                              \
+      e = launch_step_rows(m.kv_dtype == TSR_E2M1, b, p->n_items[1], s);     \
+      if (e != hipSuccess) return e;                                         \
+    }                                                                        \
+    if (p->n_merges == 0) return hipSuccess;                                 \
     hipLaunchKernelGGL((step_merge_kernel<E, D>), mgrid, dim3(256), 0, s, g); \
     return hipGetLastError();                                                \
   } while (0)

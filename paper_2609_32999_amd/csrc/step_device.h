@@ -1,0 +1,77 @@
+// Device definitions shared by the attention kernels of steps
+// (step_attn.hip: few rows, step_rows.hip: many).
+#pragma once
+
+#include <hip/hip_runtime.h>
+
+#include <cmath>
+#include <cstdint>
+
+#include "step_internal.h"
+
+namespace tsr {
+
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+
+struct StepAttnArgs {
+  const StepRow* rows;
+  const StepItem* items;
+  const int32_t* bts;
+  const void *q, *k, *v;
+  const uint8_t* scales;
+  void* out;
+  float *lse, *split_o, *split_lse;
+  int32_t n_q_heads, n_kv_heads, log2_page, window, n_sinks;
+  float scale, scale_log2e;
+};
+
+// Keys a row sees: [wlo, pos] and [lo, shi); nothing if pos < 0.
+struct Sight {
+  int32_t lo, shi, wlo, pos;
+};
+__device__ __forceinline__ Sight row_sight(const StepRow& r, int window, int n_sinks) {
+  Sight s{r.lo, r.lo + n_sinks, r.lo, r.pos};
+  if (window > 0) s.wlo = max(r.lo, r.pos - window + 1);
+  return s;
+}
+__device__ __forceinline__ bool sees(const Sight& s, int key) {
+  return (key <= s.pos) & (key >= s.lo) & ((key >= s.wlo) | (key < s.shi));
+}
+
+// A uniform 32-bit load through the scalar cache.
+__device__ __forceinline__ int32_t uniform_i32(const int32_t* p) {
+  return *reinterpret_cast<const __attribute__((address_space(4))) int32_t*>(
+      reinterpret_cast<uintptr_t>(p));
+}
+
+template <int N>
+__device__ __forceinline__ void wait_vm() {
+  asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
+}
+__device__ __forceinline__ void wait_lds() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
+
+// Direct global->LDS loads, lane l's bytes at lds + 16 l (or 4 l): base
+// uniform, `off` the lane's byte offset.  The memory clobber keeps LDS reads
+// of the buffer on their side of it.
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"
+__device__ __forceinline__ void dma16(const void* base, uint32_t off, uint32_t lds) {
+  asm volatile("s_mov_b32 m0, %2\n\tglobal_load_lds_dwordx4 %0, %1"
+               :: "v"(off), "s"(base), "s"(lds) : "m0", "memory");
+}
+__device__ __forceinline__ void dma4(const void* base, uint32_t off, uint32_t lds) {
+  asm volatile("s_mov_b32 m0, %2\n\tglobal_load_lds_dword %0, %1"
+               :: "v"(off), "s"(base), "s"(lds) : "m0", "memory");
+}
+#pragma clang diagnostic pop
+
+// Four rows x 16 columns of 16-bit values from LDS, transposed: lane i of 16
+// points at 8 bytes, row i / 4, columns 4 (i % 4) .., and receives column i.
+__device__ __forceinline__ uint2 lds_read_transposed(uint32_t at) {
+  return __builtin_bit_cast(
+      uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(uintptr_t)at));
+}
+
+}  // namespace tsr

@@ -15,6 +15,8 @@ namespace tsr {
 // Rows of an attention item times the query heads it takes: one operand of
 // a 16 x 16 matrix instruction (kernel for few rows).
 constexpr int kStepVecs = 16;
+// The same for many rows: four waves of 64.
+constexpr int kStepRowVecs = 256;
 // Keys per tile: two 16-key blocks, each within one page (bf16, e2m1).
 constexpr int kStepKeys = 32;
 
@@ -41,19 +43,22 @@ struct alignas(16) StepItem {
   int32_t kv_len;
   int32_t a0, a1, b0, b1;
   int32_t full_lo, full_hi;
-  int32_t part_slot;  // -1: writes out and lse, else its split buffer slot
+  int32_t part_slot;  // -1: writes out and lse, else its first vector in the split buffer
   int32_t pad[2];
 };
 
-// A split item: its ranges are slots slot0 .. slot0 + n_slots - 1.
+// 16 vectors of an item whose key range was cut: vectors vec0 .. vec0 + 15 of
+// the item (rows row0 .., n_heads heads from hq0 on); range c's are at vector
+// slot0 + c * stride of the split buffer.
 struct alignas(16) StepMerge {
   int32_t row0;
   int32_t n_rows;
-  int32_t hq0;       // first query head
+  int32_t hq0;
   int32_t n_heads;
   int32_t slot0;
   int32_t n_slots;
-  int32_t pad[2];
+  int32_t stride;
+  int32_t vec0;
 };
 
 // A page of the requests and how many of its slots hold positions.
@@ -64,12 +69,12 @@ struct alignas(8) StepPage {
 
 struct StepDev {
   const StepRow* rows;
-  const StepItem* items;
+  const StepItem* items;       // for few rows, then for many
   const StepMerge* merges;
   const StepPage* pages;
   const int32_t* bts;
-  float* split_o;    // [slots][vecs][head_dim], normalised
-  float* split_lse;  // [slots][vecs], natural log
+  float* split_o;    // [vectors][head_dim], normalised
+  float* split_lse;  // [vectors], natural log
   const float* rope_cos;
   const float* rope_sin;
 };
@@ -80,8 +85,10 @@ struct tsr_step {
   tsr_model model;
   tsr_step_options opt;
   float scale;
-  int32_t T, n_items, n_merges, n_pages, n_req_pages;
-  int32_t item_vecs;       // rows x heads of an item
+  int32_t T, n_pages, n_req_pages;
+  int32_t n_items[2];      // launch sizes: few rows, many rows (with padding)
+  int32_t n_real_items;    // both, without
+  int32_t n_split_items, n_merges;
   bool shared_append;      // a row's page belongs to another request too
   size_t image_bytes, ws_bytes;
   size_t off_rows, off_items, off_merges, off_pages, off_bts, off_split_o, off_split_lse;
@@ -105,6 +112,8 @@ hipError_t launch_step_pack(const tsr_step* p, const void* bf16_k, const void* b
                             void* req_k, void* req_v, void* req_scale, hipStream_t s);
 hipError_t launch_step_unpack(const tsr_step* p, const void* req_k, const void* req_v,
                               const void* req_scale, void* bf16_k, void* bf16_v, hipStream_t s);
+struct StepAttnArgs;
+hipError_t launch_step_rows(bool four_bit, const StepAttnArgs& a, int n_items, hipStream_t s);
 hipError_t launch_step_attn(const tsr_step* p, const void* q, const void* req_k,
                             const void* req_v, const void* req_scale, void* out, float* lse,
                             hipStream_t s);

@@ -1,6 +1,7 @@
 // Steps of tsr_step.h on the host: validation, the row and attention item
 // lists, and the entry points.  Every check runs before anything is enqueued.
 #include <algorithm>
+#include <array>
 #include <cmath>
 #include <cstring>
 #include <initializer_list>
@@ -23,11 +24,14 @@ tsr_status fail_req(tsr_status st, int r, const std::string& msg) {
   return fail(st, "request " + std::to_string(r) + ": " + msg);
 }
 
-// Compute units and key ranges: a launch is cut into about this many items
-// a compute unit, of kMinRangeTiles tiles at least.
+// A launch for few rows is cut into about this many items a compute unit, of
+// kMinRangeTiles tiles at least; one for many rows into one a unit.
 constexpr int kRangesPerCu = 2;
 constexpr int kMinRangeTiles = 8;
-constexpr int kMaxStepSlots = 1 << 16;
+constexpr int kMinRowRangeTiles = 16;
+constexpr int64_t kMaxSplitVecs = (int64_t)1 << 21;
+// Requests with this many rows x heads go to the kernel for many rows.
+constexpr int kManyVecs = 64;
 
 // Key tiles [a0, a1) and [b0, b1) that hold every key some row of
 // rows[r0 .. r0 + n) sees, and the keys visible to all of them.
@@ -86,6 +90,30 @@ StepItem cut(const StepItem& it, int32_t t0, int32_t t1) {
   return c;
 }
 
+// Launch order: workgroups go to the XCDs in turn, so the list, in which
+// items that share keys are neighbours, is cut into one run of equal work for
+// each XCD and its cache; within a run the longest items start first.
+void schedule(const std::vector<StepItem>& list, std::vector<StepItem>* out) {
+  std::array<std::vector<StepItem>, kNumXcd> run;
+  auto cost = [](const StepItem& it) { return (int64_t)n_tiles(it) + 2; };
+  int64_t total = 0, at = 0;
+  for (const StepItem& it : list) total += cost(it);
+  for (const StepItem& it : list) {
+    const int64_t mid = at + cost(it) / 2;
+    run[std::min<int64_t>(kNumXcd - 1, mid * kNumXcd / total)].push_back(it);
+    at += cost(it);
+  }
+  size_t most = 0;
+  for (auto& r : run) {
+    std::stable_sort(r.begin(), r.end(), [](const StepItem& a, const StepItem& b) {
+      return n_tiles(a) > n_tiles(b);
+    });
+    most = std::max(most, r.size());
+  }
+  for (size_t i = 0; i < most; ++i)
+    for (const auto& r : run) out->push_back(i < r.size() ? r[i] : StepItem{});
+}
+
 tsr_status build_step(const tsr_model* model, const tsr_step_request* reqs, int32_t n_req,
                       int32_t n_req_pages, const tsr_step_options* options, tsr_step* p) {
   tsr_status st = check_step_model(model);
@@ -101,6 +129,8 @@ tsr_status build_step(const tsr_model* model, const tsr_step_request* reqs, int3
     return fail(TSR_ERR_INVALID_ARG, "tsr_step_options.split_tiles must be -1, 0 or positive");
   if (o.attn_kernel < 0 || o.attn_kernel > 2)
     return fail(TSR_ERR_INVALID_ARG, "tsr_step_options.attn_kernel must be 0, 1 or 2");
+  if (o.attn_kernel == 2 && m.act_dtype != TSR_BF16)
+    return fail(TSR_ERR_UNSUPPORTED, "attn_kernel 2 is built for bf16 activations only");
   if (n_req < 0 || (n_req > 0 && !reqs))
     return fail(TSR_ERR_INVALID_ARG, "n_req < 0, or reqs is NULL");
   if (n_req_pages < 0) return fail(TSR_ERR_INVALID_ARG, "n_req_pages must be >= 0");
@@ -182,74 +212,79 @@ tsr_status build_step(const tsr_model* model, const tsr_step_request* reqs, int3
   for (int32_t i = 0; i < n_req_pages; ++i)
     if (page_n[i]) pages.push_back({i, page_n[i]});
 
-  // attention items: row tile x head block x KV head
-  p->item_vecs = kStepVecs;
-  const int hb = std::min(G, kStepVecs);              // heads of an item
-  const int rt = std::max(1, kStepVecs / hb);         // rows of an item
-  std::vector<StepItem> whole;
-  for (int r = 0; r < n_req; ++r)
-    for (int i = row0[r]; i < row0[r + 1]; i += rt) {
-      StepItem it{};
-      it.row0 = i;
-      it.n_rows = std::min(rt, row0[r + 1] - i);
-      it.bt_off = bt_off[r];
-      it.kv_len = reqs[r].kv_len;
-      it.part_slot = -1;
-      item_keys(rows, i, it.n_rows, o, &it);
-      for (int g = 0; g < Hkv; ++g)
-        for (int h = 0; h < G; h += hb) {
+  // attention items: row tile x head block x KV head, of either kernel
+  std::vector<StepItem> whole[2];
+  for (int r = 0; r < n_req; ++r) {
+    const int64_t vecs = (int64_t)(row0[r + 1] - row0[r]) * G;
+    const int kind = o.attn_kernel ? o.attn_kernel - 1
+                                   : m.act_dtype == TSR_BF16 && vecs >= kManyVecs;
+    const int most = kind ? kStepRowVecs : kStepVecs;
+    const int hb = std::min(G, most);              // heads of an item
+    const int rt = most / hb;                      // rows of an item
+    for (int g = 0; g < Hkv; ++g)
+      for (int h = 0; h < G; h += hb)
+        for (int i = row0[r]; i < row0[r + 1]; i += rt) {
+          StepItem it{};
+          it.row0 = i;
+          it.n_rows = std::min(rt, row0[r + 1] - i);
+          it.bt_off = bt_off[r];
+          it.kv_len = reqs[r].kv_len;
+          it.part_slot = -1;
           it.kv_head = g;
           it.head0 = h;
           it.n_heads = std::min(hb, G - h);
-          whole.push_back(it);
+          item_keys(rows, i, it.n_rows, o, &it);
+          whole[kind].push_back(it);
         }
-    }
-  if (whole.size() > (size_t)INT32_MAX / 4)
+  }
+  if (whole[0].size() + whole[1].size() > (size_t)INT32_MAX / 64)
     return fail(TSR_ERR_OUT_OF_RANGE, "too many attention items");
 
-  // key ranges
-  int64_t total = 0;
-  for (const StepItem& it : whole) total += n_tiles(it);
-  int64_t cap = INT32_MAX;
-  if (o.split_tiles > 0) cap = o.split_tiles;
-  if (o.split_tiles == 0) {
-    const int64_t want = (int64_t)kRangesPerCu * kNumCus;
-    cap = std::max<int64_t>(kMinRangeTiles, (total + want - 1) / want);
-  }
   std::vector<StepItem> items;
   std::vector<StepMerge> merges;
-  int64_t slots = 0;
-  for (const StepItem& it : whole) {
-    const int64_t n = n_tiles(it);
-    int64_t parts = std::max<int64_t>(1, (n + cap - 1) / cap);
-    if (parts > 1 && slots + parts > kMaxStepSlots) {
-      if (o.split_tiles > 0)
-        return fail(TSR_ERR_OUT_OF_RANGE, "split_tiles cuts this step into too many ranges");
-      parts = 1;
+  int64_t split_vecs = 0;
+  p->n_split_items = p->n_real_items = 0;
+  for (int kind = 0; kind < 2; ++kind) {
+    const int most = kind ? kStepRowVecs : kStepVecs;
+    // key ranges
+    int64_t total = 0;
+    for (const StepItem& it : whole[kind]) total += n_tiles(it);
+    int64_t cap = INT32_MAX;
+    if (o.split_tiles > 0) cap = o.split_tiles;
+    if (o.split_tiles == 0) {
+      const int64_t want = (int64_t)(kind ? 1 : kRangesPerCu) * kNumCus;
+      cap = std::max<int64_t>(kind ? kMinRowRangeTiles : kMinRangeTiles,
+                              (total + want - 1) / want);
     }
-    if (parts == 1) {
-      items.push_back(it);
-      continue;
+    std::vector<StepItem> list;
+    for (const StepItem& it : whole[kind]) {
+      const int64_t n = n_tiles(it);
+      int64_t parts = std::max<int64_t>(1, (n + cap - 1) / cap);
+      if (parts > 1 && split_vecs + parts * most > kMaxSplitVecs) {
+        if (o.split_tiles > 0)
+          return fail(TSR_ERR_OUT_OF_RANGE, "split_tiles cuts this step into too many ranges");
+        parts = 1;
+      }
+      if (parts == 1) {
+        list.push_back(it);
+        continue;
+      }
+      ++p->n_split_items;
+      for (int v = 0; v < it.n_rows * it.n_heads; v += kStepVecs)
+        merges.push_back({it.row0, it.n_rows, it.kv_head * G + it.head0, it.n_heads,
+                          (int32_t)split_vecs + v, (int32_t)parts, most, v});
+      for (int64_t c = 0; c < parts; ++c) {
+        StepItem x = cut(it, (int32_t)(n * c / parts), (int32_t)(n * (c + 1) / parts));
+        x.part_slot = (int32_t)(split_vecs + c * most);
+        list.push_back(x);
+      }
+      split_vecs += parts * most;
     }
-    StepMerge mg{};
-    mg.row0 = it.row0;
-    mg.n_rows = it.n_rows;
-    mg.hq0 = it.kv_head * G + it.head0;
-    mg.n_heads = it.n_heads;
-    mg.slot0 = (int32_t)slots;
-    mg.n_slots = (int32_t)parts;
-    merges.push_back(mg);
-    for (int64_t c = 0; c < parts; ++c) {
-      StepItem x = cut(it, (int32_t)(n * c / parts), (int32_t)(n * (c + 1) / parts));
-      x.part_slot = (int32_t)slots++;
-      items.push_back(x);
-    }
+    p->n_real_items += (int32_t)list.size();
+    const size_t before = items.size();
+    schedule(list, &items);
+    p->n_items[kind] = (int32_t)(items.size() - before);
   }
-  // longest first: the launch ends with its short items
-  std::stable_sort(items.begin(), items.end(), [](const StepItem& a, const StepItem& b) {
-    return n_tiles(a) > n_tiles(b);
-  });
-  p->n_items = (int32_t)items.size();
   p->n_merges = (int32_t)merges.size();
   p->n_pages = (int32_t)pages.size();
 
@@ -266,8 +301,8 @@ tsr_status build_step(const tsr_model* model, const tsr_step_request* reqs, int3
   p->off_bts = place(bts.size() * sizeof(int32_t));
   p->image_bytes = std::max<size_t>(off, 256);
   // the split buffer is written by the kernels, not uploaded
-  p->off_split_o = place((size_t)slots * p->item_vecs * m.head_dim * sizeof(float));
-  p->off_split_lse = place((size_t)slots * p->item_vecs * sizeof(float));
+  p->off_split_o = place((size_t)split_vecs * m.head_dim * sizeof(float));
+  p->off_split_lse = place((size_t)split_vecs * sizeof(float));
   p->ws_bytes = std::max<size_t>(off, 256);
   p->image.assign(p->image_bytes, 0);
   auto put = [&](size_t at, const void* src, size_t bytes) {
@@ -397,9 +432,11 @@ tsr_status tsr_step_create(const tsr_model* model, const tsr_step_request* reqs,
 void tsr_step_destroy(tsr_step* p) { delete p; }
 
 int32_t tsr_step_num_rows(const tsr_step* p) { return p ? p->T : -1; }
-int32_t tsr_step_num_attn_items(const tsr_step* p) { return p ? p->n_items : -1; }
-int32_t tsr_step_num_attn_splits(const tsr_step* p) { return p ? p->n_merges : -1; }
-int32_t tsr_step_attn_item_rows(const tsr_step* p) { return p ? p->item_vecs : -1; }
+int32_t tsr_step_num_attn_items(const tsr_step* p) { return p ? p->n_real_items : -1; }
+int32_t tsr_step_num_attn_splits(const tsr_step* p) { return p ? p->n_split_items : -1; }
+int32_t tsr_step_attn_item_rows(const tsr_step* p) {
+  return !p ? -1 : p->n_items[1] ? kStepRowVecs : kStepVecs;
+}
 
 tsr_status tsr_step_append(const tsr_step* p, const tsr_qk_norm* norm, const void* q,
                            int64_t q_stride, const void* k, int64_t k_stride, const void* v,

@@ -1,0 +1,473 @@
+// Attention of a step's rows over request pages (tsr_step.h), for many rows
+// per request: extensions and prefills, bf16 and 4-bit pages.
+//
+// Bound by the matrix cores, and before them by LDS: a K or V fragment read
+// from LDS feeds one 32x32x16 product a block of 32 vectors (rows x heads), 32
+// cycles of a SIMD for 1 KB, and four SIMDs share 128 bytes a cycle.  So a
+// wave owns two blocks, 64 vectors, and uses every fragment twice; a workgroup
+// of four waves, 256 vectors, stages each 32-key tile once for all of them.
+//   S^T = K Q^T     v_mfma_f32_32x32x16_bf16
+//   online softmax  fp32, lane-local but for one exchange (a lane holds one
+//                   vector of each block, and half its keys)
+//   O^T += V^T P^T  v_mfma_f32_32x32x16_f16
+// P and V enter the second product as fp16: rounding P to bf16 would put as
+// much error on an output as its own rounding, fp16 an eighth of it.  K goes
+// straight to LDS in operand order (4-bit K through registers, as bf16); V
+// through registers to fp16 rows, whose 16-byte chunks are permuted by the key
+// so that the transposing reads of V^T touch every bank once.
+#include <type_traits>
+
+#include "attn_common.h"
+#include "e2m1.h"
+#include "kernels_common.h"
+#include "step_device.h"
+
+namespace tsr {
+
+namespace {
+
+constexpr int kRowWaves = 4;
+constexpr int kRowBytes = 2 * kD;   // a key's K or V row in LDS
+constexpr int kTileBytes = kStepKeys * kRowBytes;
+
+// K buffers; bytes of a wave's own space for a tile; direct loads a wave issues
+// for a tile; 16-byte runs of V a lane converts.
+template <bool F4> struct Staging;
+template <> struct Staging<false> {
+  static constexpr int kKBufs = 3, kRaw = 2048, kLoads = 4, kVRuns = 2;
+};
+template <> struct Staging<true> {
+  static constexpr int kKBufs = 2, kRaw = 1280, kLoads = 2, kVRuns = 4;
+};
+
+__device__ __forceinline__ uint32_t bf16x2_to_f16x2(uint32_t w) {
+  const f16x2 h = {(_Float16)__uint_as_float(w << 16),
+                   (_Float16)__uint_as_float(w & 0xffff0000u)};
+  return __builtin_bit_cast(uint32_t, h);
+}
+// Nonzero if one of the two fp16 values is infinite or NaN.
+__device__ __forceinline__ uint32_t f16x2_not_finite(uint32_t w) {
+  return ((w & 0x7c007c00u) + 0x04000400u) & 0x80008000u;
+}
+__device__ __forceinline__ uint32_t finite_or_0(uint32_t w) {
+  const uint32_t off = f16x2_not_finite(w) >> 15;   // bits 0 and 16
+  return w & ~(off * 0xffffu);
+}
+
+template <bool F4>
+__global__ __launch_bounds__(64 * kRowWaves, 1) void step_rows_kernel(const StepAttnArgs a) {
+  using S = Staging<F4>;
+  __shared__ __attribute__((aligned(1024))) uint8_t kl[S::kKBufs * kTileBytes];
+  __shared__ __attribute__((aligned(1024))) uint8_t vl[2 * kTileBytes];
+  __shared__ __attribute__((aligned(1024))) uint8_t raw[kRowWaves * 2 * S::kRaw];
+  __shared__ Sight sights[kStepRowVecs];
+  __shared__ uint32_t bad_v[kRowWaves];   // wave w replaced values that are not finite
+
+  const StepItem it = a.items[blockIdx.x];
+  if (it.n_rows == 0) return;
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int l32 = lane & 31, lh = lane >> 5, c16 = lane & 15;
+  const int G = a.n_q_heads / a.n_kv_heads;
+  const int page_mask = (1 << a.log2_page) - 1;
+  const int32_t* bt = a.bts + it.bt_off;
+
+  const int na = it.a1 - it.a0, nt = na + it.b1 - it.b0;
+  auto tile_key = [&](int t) { return kStepKeys * (t < na ? it.a0 + t : it.b0 + t - na); };
+  const int last = it.kv_len - 1, last_blk = last & ~15;
+
+  // ---- staging, two tiles ahead.  Wave w serves 16-key block w / 2 of a tile:
+  //   bf16   K's 32-dim runs 2 (w % 2) .. + 1, by direct loads into place, and
+  //          V's keys 8 (w % 2) .. + 7, by direct loads into the wave's own
+  //          space, from where they go on as fp16 rows a tile later;
+  //   4-bit  K (w even) or V (odd): codes and scales into the wave's own space.
+  // Keys past the last one read it again (as in step_attn.hip).
+  const int sb = w >> 1, half = w & 1;
+  int page = 0;
+  auto fetch_page = [&](int t) {
+    page = uniform_i32(bt + (min(tile_key(t) + 16 * sb, last_blk) >> a.log2_page));
+  };
+  uint8_t* const mine = raw + w * (2 * S::kRaw);
+  const int skey = 8 * half + (lane >> 4);   // bf16 V: this key and the one 4 on
+  auto issue = [&](int t) __attribute__((always_inline)) {
+    const int kb = min(tile_key(t) + 16 * sb, last_blk);
+    const int top = last - kb;
+    const int64_t slot = ((((int64_t)page * a.n_kv_heads + it.kv_head) << a.log2_page) +
+                          (kb & page_mask));
+    const uint32_t own = lds_addr(mine) + (t & 1) * S::kRaw;
+    if constexpr (!F4) {
+      const uint8_t* kp = static_cast<const uint8_t*>(a.k) + slot * kRowBytes;
+      const uint8_t* vp = static_cast<const uint8_t*>(a.v) + slot * kRowBytes;
+      const uint32_t dst = lds_addr(kl) + (t % S::kKBufs) * kTileBytes + 4096 * sb + 2048 * half;
+      const uint32_t ko = min(c16, top) * kRowBytes + 128 * half + 16 * (lane >> 4);
+      dma16(kp, ko, dst);
+      dma16(kp, ko + 64, dst + 1024);
+      dma16(vp, min(skey, top) * kRowBytes + 16 * c16, own);
+      dma16(vp, min(skey + 4, top) * kRowBytes + 16 * c16, own + 1024);
+    } else {
+      const uint8_t* cp = static_cast<const uint8_t*>(half ? a.v : a.k) + slot * (kD / 2);
+      const int64_t ss = ((((int64_t)page * 2 + half) * a.n_kv_heads + it.kv_head)
+                          << a.log2_page) + (kb & page_mask);
+      const int kk = min(c16, top);
+      dma16(cp, kk * (kD / 2) + 16 * (lane >> 4), own);
+      dma4(a.scales + ss * (kD / kScaleDims), kk * (kD / kScaleDims), own + 1024);
+    }
+  };
+  // fp16 values of V in tiles that not every row sees in full: a masked key
+  // weighs 0, but 0 x inf is not 0, so values that are not finite are 0 there,
+  // and the rows that see them get them at the end
+  auto clean = [&](uint4 (&x)[S::kVRuns]) __attribute__((always_inline)) {
+    uint32_t off = 0;
+#pragma unroll
+    for (int e = 0; e < S::kVRuns; ++e)
+      off |= f16x2_not_finite(x[e].x) | f16x2_not_finite(x[e].y) | f16x2_not_finite(x[e].z) |
+             f16x2_not_finite(x[e].w);
+    if (__builtin_amdgcn_ballot_w64(off != 0)) {
+      if (lane == 0) bad_v[w] = 1;
+#pragma unroll
+      for (int e = 0; e < S::kVRuns; ++e)
+        x[e] = make_uint4(finite_or_0(x[e].x), finite_or_0(x[e].y), finite_or_0(x[e].z),
+                          finite_or_0(x[e].w));
+    }
+  };
+  // the wave's part of tile t, from its own space on
+  auto convert = [&](int t) __attribute__((always_inline)) {
+    const int key0 = tile_key(t);
+    const bool masked = key0 < it.full_lo || key0 + kStepKeys - 1 > it.full_hi;
+    const uint8_t* own = mine + (t & 1) * S::kRaw;
+    uint8_t* vt = vl + (t & 1) * kTileBytes;
+    uint4 x[S::kVRuns];
+    if constexpr (!F4) {
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        const uint4 r = *reinterpret_cast<const uint4*>(own + 1024 * e + 16 * lane);
+        x[e] = make_uint4(bf16x2_to_f16x2(r.x), bf16x2_to_f16x2(r.y), bf16x2_to_f16x2(r.z),
+                          bf16x2_to_f16x2(r.w));
+      }
+      if (masked) clean(x);
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        const int key = 16 * sb + skey + 4 * e;
+        *reinterpret_cast<uint4*>(vt + key * kRowBytes + 16 * (c16 ^ (2 * (key & 7)))) = x[e];
+      }
+    } else {
+      // this lane's key c16 and 32 dims
+      const uint4 r = *reinterpret_cast<const uint4*>(own + 16 * lane);
+      const float f = e2m1_factor(own[1024 + 4 * c16 + (lane >> 4)]);
+      const uint32_t c[4] = {r.x, r.y, r.z, r.w};
+#pragma unroll
+      for (int e = 0; e < 4; ++e) x[e] = e2m1_decode8(c[e], f);
+      if (!half) {
+        uint8_t* kt = kl + (t % S::kKBufs) * kTileBytes + 4096 * sb + 1024 * (lane >> 4);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) *reinterpret_cast<uint4*>(kt + 256 * e + 16 * c16) = x[e];
+      } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          x[e] = make_uint4(bf16x2_to_f16x2(x[e].x), bf16x2_to_f16x2(x[e].y),
+                            bf16x2_to_f16x2(x[e].z), bf16x2_to_f16x2(x[e].w));
+        if (masked) clean(x);
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          *reinterpret_cast<uint4*>(vt + (16 * sb + c16) * kRowBytes +
+                                    16 * ((4 * (lane >> 4) + e) ^ (2 * (c16 & 7)))) = x[e];
+      }
+    }
+  };
+
+  if (tid < kRowWaves) bad_v[tid] = 0;
+  if (nt > 0) {
+    fetch_page(0);
+    issue(0);
+  }
+  if (nt > 1) {
+    fetch_page(1);
+    issue(1);
+  }
+  if (nt > 2) fetch_page(2);
+
+  // ---- this wave's vectors: v = 64 w + 32 b + l32 is row v / heads, head v %
+  // heads of the item; vectors past the last repeat the last row
+  Frag qf[2][8];
+  // keys [seen_lo, seen_hi] hold all that the wave's rows see beside the sinks
+  // [0, sink_hi); [full_lo, full_hi] is seen by all of them
+  int seen_lo = INT32_MAX, seen_hi = -1, sink_hi = 0, full_lo = 0, full_hi = INT32_MAX;
+#pragma unroll
+  for (int b = 0; b < 2; ++b) {
+    const int v = 64 * w + 32 * b + l32;
+    int r = v / it.n_heads, h = v - r * it.n_heads;
+    if (r >= it.n_rows) {
+      r = it.n_rows - 1;
+      h = 0;
+    }
+    const StepRow row = a.rows[it.row0 + r];
+    const Sight sight = row_sight(row, a.window, a.n_sinks);
+    if (lh == 0) sights[v] = sight;   // read by this wave alone
+    const uint16_t* qp = static_cast<const uint16_t*>(a.q) +
+                         ((int64_t)(it.row0 + r) * a.n_q_heads + it.kv_head * G + it.head0 + h) *
+                             kD;
+#pragma unroll
+    for (int k = 0; k < 8; ++k)
+      qf[b][k].u = *reinterpret_cast<const uint4*>(qp + 16 * k + 8 * lh);
+    const bool some = row.pos >= 0 && row.lo <= row.pos;
+    if (some) {
+      seen_lo = min(seen_lo, sight.wlo);
+      seen_hi = max(seen_hi, row.pos);
+      sink_hi = max(sink_hi, min(sight.shi, sight.wlo));
+    }
+    full_lo = max(full_lo, sight.wlo);
+    full_hi = min(full_hi, some ? row.pos : -1);
+  }
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) {
+    seen_lo = min(seen_lo, __shfl_xor(seen_lo, o));
+    seen_hi = max(seen_hi, __shfl_xor(seen_hi, o));
+    sink_hi = max(sink_hi, __shfl_xor(sink_hi, o));
+    full_lo = max(full_lo, __shfl_xor(full_lo, o));
+    full_hi = min(full_hi, __shfl_xor(full_hi, o));
+  }
+  seen_lo = __builtin_amdgcn_readfirstlane(seen_lo);
+  seen_hi = __builtin_amdgcn_readfirstlane(seen_hi);
+  sink_hi = __builtin_amdgcn_readfirstlane(sink_hi);
+  full_lo = __builtin_amdgcn_readfirstlane(full_lo);
+  full_hi = __builtin_amdgcn_readfirstlane(full_hi);
+  const bool active = 64 * w < it.n_rows * it.n_heads;
+
+  f32x16 o[2][4];
+#pragma unroll
+  for (int b = 0; b < 2; ++b)
+#pragma unroll
+    for (int db = 0; db < 4; ++db)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) o[b][db][r] = 0.0f;
+  float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.0f, 0.0f};
+  // Q in accumulation registers, where only the matrix instructions read it;
+  // all of it here before the loop, whose waits are for the next tiles
+#pragma unroll
+  for (int b = 0; b < 2; ++b)
+#pragma unroll
+    for (int k = 0; k < 8; ++k) asm volatile("" : "+a"(qf[b][k].b));
+  const float sc = a.scale_log2e;
+  // operand reads: K fragment k at kfl + (k / 2) 1024 + (k % 2) 512; V^T
+  // fragment (16 keys h, 32 dims db) at (vfl ^ 64 db) + 4096 h, + 2048
+  const uint32_t kfl = 4096 * (l32 >> 4) + 256 * lh + 16 * c16;
+  const int tk = 4 * lh + (c16 >> 2);
+  const uint32_t vfl = tk * kRowBytes + 32 * (((lane >> 4) & 1) ^ (tk & 7)) + 8 * (c16 & 3);
+
+  // One tile.  With one wave on a SIMD nothing else hides the softmax, so the
+  // two blocks go through it half a tile apart: block 0's under the QK^T
+  // products of block 1, block 1's under the PV products of block 0.
+  auto tile = [&](int key0, auto mask_tag, const uint8_t* kt, const uint8_t* vt)
+      __attribute__((always_inline)) {
+    constexpr bool MASK = decltype(mask_tag)::value;
+    f32x16 s[2];
+    f16x8 pf[2][2];
+    float lt[2];
+    auto scores = [&](int b, const Frag (&kf)[8]) __attribute__((always_inline)) {
+#pragma unroll
+      for (int r = 0; r < 16; ++r) s[b][r] = 0.0f;
+#pragma unroll
+      for (int k = 0; k < 8; ++k)
+        s[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[k].b, qf[b][k].b, s[b], 0, 0, 0);
+    };
+    auto probabilities = [&](int b) __attribute__((always_inline)) {
+      const float mc = m[b] == -INFINITY ? 0.0f : m[b] * sc;
+      float ls[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        const float p = __builtin_amdgcn_exp2f(fmaf(s[b][r], sc, -mc));
+        ls[r & 3] += p;
+        pf[b][r >> 3][r & 7] = (_Float16)p;
+      }
+      lt[b] = (ls[0] + ls[1]) + (ls[2] + ls[3]);
+    };
+    auto softmax = [&](int b) __attribute__((always_inline)) {
+      if constexpr (MASK) {
+        const Sight sight = sights[64 * w + 32 * b + l32];
+#pragma unroll
+        for (int r = 0; r < 16; ++r)
+          s[b][r] = sees(sight, key0 + 8 * (r >> 2) + 4 * lh + (r & 3)) ? s[b][r] : -INFINITY;
+      }
+      probabilities(b);
+    };
+    // the running maximum moves only when the probabilities taken against it
+    // grow past 2^kLazy, or while it is -inf
+    auto settle = [&](int b) __attribute__((always_inline)) {
+      if (__builtin_amdgcn_ballot_w64(!(lt[b] <= kLazySum) || m[b] == -INFINITY)) {
+        float big = -INFINITY;
+#pragma unroll
+        for (int r = 0; r < 16; ++r) big = fmaxf(big, s[b][r]);
+        big = fmaxf(big, __shfl_xor(big, 32));
+        const float mn = fmaxf(m[b], big);
+        const float alpha = mn == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f((m[b] - mn) * sc);
+        m[b] = mn;
+        l[b] *= alpha;
+#pragma unroll
+        for (int db = 0; db < 4; ++db)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) o[b][db][r] *= alpha;
+        probabilities(b);
+      }
+      l[b] += lt[b];
+    };
+    Frag vf[2][4];
+    auto outputs = [&](int b) __attribute__((always_inline)) {
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int db = 0; db < 4; ++db)
+          o[b][db] = __builtin_amdgcn_mfma_f32_32x32x16_f16(vf[h][db].h, pf[b][h], o[b][db], 0, 0, 0);
+    };
+    {
+      Frag kf[8];
+#pragma unroll
+      for (int k = 0; k < 8; ++k)
+        kf[k].u = *reinterpret_cast<const uint4*>(kt + kfl + 1024 * (k >> 1) + 512 * (k & 1));
+      scores(0, kf);
+      scores(1, kf);
+    }
+    softmax(0);
+    settle(0);
+    const uint32_t va = lds_addr(vt) + vfl;
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+      for (int db = 0; db < 4; ++db) {
+        const uint2 x = lds_read_transposed((va ^ (64 * db)) + 4096 * h);
+        const uint2 y = lds_read_transposed((va ^ (64 * db)) + 4096 * h + 2048);
+        vf[h][db].u = make_uint4(x.x, x.y, y.x, y.y);
+      }
+    outputs(0);
+    softmax(1);
+    settle(1);
+    outputs(1);
+  };
+
+  // (the queries' wait above was for the first tiles too)
+  if (nt > 0) convert(0);
+  __syncthreads();
+  for (int t = 0; t < nt; ++t) {
+    if (t + 2 < nt) {
+      wait_lds();   // the space it goes to has been read
+      issue(t + 2);
+      if (t + 3 < nt) fetch_page(t + 3);
+    }
+    const int key0 = tile_key(t);
+    const uint8_t* kt = kl + (t % S::kKBufs) * kTileBytes;
+    const uint8_t* vt = vl + (t & 1) * kTileBytes;
+    if (active && ((key0 <= seen_hi && key0 + kStepKeys > seen_lo) || key0 < sink_hi)) {
+      if (key0 < full_lo || key0 + kStepKeys - 1 > full_hi)
+        tile(key0, std::true_type{}, kt, vt);
+      else
+        tile(key0, std::false_type{}, kt, vt);
+    }
+    if (t + 1 < nt) {
+      if (t + 2 < nt)
+        wait_vm<S::kLoads>();
+      else
+        wait_vm<0>();
+      convert(t + 1);
+    }
+    __syncthreads();
+  }
+
+  if (!active) return;
+  // ---- values that are not finite, for the rows that see them
+  if (bad_v[0] | bad_v[1] | bad_v[2] | bad_v[3]) {
+#pragma unroll 1
+    for (int t = 0; t < nt; ++t) {
+      const int key0 = tile_key(t);
+      if (key0 >= it.full_lo && key0 + kStepKeys - 1 <= it.full_hi) continue;
+#pragma unroll 1
+      for (int j = key0; j < min(key0 + kStepKeys, it.kv_len); ++j) {
+        const int64_t page = bt[j >> a.log2_page];
+        const int64_t slot = ((page * a.n_kv_heads + it.kv_head) << a.log2_page) + (j & page_mask);
+        const int64_t scale = ((((2 * page + 1) * a.n_kv_heads + it.kv_head) << a.log2_page) +
+                               (j & page_mask)) * (kD / kScaleDims);
+        const bool see[2] = {sees(sights[64 * w + l32], j), sees(sights[64 * w + 32 + l32], j)};
+#pragma unroll
+        for (int db = 0; db < 4; ++db)
+#pragma unroll
+          for (int x = 0; x < 4; ++x) {
+            const int d = 32 * db + 8 * x + 4 * lh;
+            uint2 u;
+            if constexpr (F4) {
+              const uint32_t c = *reinterpret_cast<const uint16_t*>(
+                  static_cast<const uint8_t*>(a.v) + slot * (kD / 2) + d / 2);
+              const uint4 y = e2m1_decode8(c, e2m1_factor(a.scales[scale + db]));
+              u = make_uint2(y.x, y.y);
+            } else {
+              u = *reinterpret_cast<const uint2*>(static_cast<const uint16_t*>(a.v) + slot * kD + d);
+            }
+            const uint32_t f[2] = {bf16x2_to_f16x2(u.x), bf16x2_to_f16x2(u.y)};
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              const float y = (float)__builtin_bit_cast(f16x2, f[e >> 1])[e & 1];
+              if (fabsf(y) <= 65504.0f) continue;
+#pragma unroll
+              for (int b = 0; b < 2; ++b)
+                if (see[b]) o[b][db][4 * x + e] += y;
+            }
+          }
+      }
+    }
+  }
+
+  // ---- out
+#pragma unroll
+  for (int b = 0; b < 2; ++b) {
+    const float lt = l[b] + __shfl_xor(l[b], 32);
+    const int v0 = 64 * w + 32 * b, v = v0 + l32;
+    const int n_vecs = it.n_rows * it.n_heads;
+    const int n_mine = min(32, n_vecs - v0);
+    if (n_mine <= 0) continue;
+    const Sight sight = sights[v];
+    const float ls = m[b] * a.scale + logf(lt);
+    if (it.part_slot >= 0) {
+      const bool none = lt == 0.0f;
+      const float inv = none ? 0.0f : 1.0f / lt;
+      if (v < n_vecs) {
+        const int64_t at = (int64_t)it.part_slot + v;
+#pragma unroll
+        for (int db = 0; db < 4; ++db)
+#pragma unroll
+          for (int x = 0; x < 4; ++x)
+            *reinterpret_cast<float4*>(a.split_o + at * kD + 32 * db + 8 * x + 4 * lh) =
+                make_float4(o[b][db][4 * x] * inv, o[b][db][4 * x + 1] * inv,
+                            o[b][db][4 * x + 2] * inv, o[b][db][4 * x + 3] * inv);
+        if (lh == 0) a.split_lse[at] = none ? -INFINITY : ls;
+      }
+      continue;
+    }
+    const bool empty = sight.pos < 0 || sight.lo > sight.pos;
+    float inv = 1.0f / lt;
+    if (empty) {
+      inv = 1.0f;
+#pragma unroll
+      for (int db = 0; db < 4; ++db)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) o[b][db][r] = 0.0f;
+    }
+    auto vec_row = [&](int i) -> int64_t {
+      const int r = (v0 + i) / it.n_heads, h = v0 + i - r * it.n_heads;
+      return (int64_t)(it.row0 + r) * a.n_q_heads + it.kv_head * G + it.head0 + h;
+    };
+    if (a.lse && lh == 0 && l32 < n_mine) a.lse[vec_row(l32)] = empty ? -INFINITY : ls;
+    // (every wave is past the last tile's barrier: K's buffer is free)
+    store_out(o[b], inv, kl + w * kOutLds, lane, n_mine, static_cast<uint16_t*>(a.out),
+              [&](int i) -> int64_t { return vec_row(i) * kD; });
+  }
+}
+
+}  // namespace
+
+hipError_t launch_step_rows(bool four_bit, const StepAttnArgs& a, int n_items, hipStream_t s) {
+  const dim3 grid(n_items), block(64 * kRowWaves);
+  if (four_bit)
+    hipLaunchKernelGGL(step_rows_kernel<true>, grid, block, 0, s, a);
+  else
+    hipLaunchKernelGGL(step_rows_kernel<false>, grid, block, 0, s, a);
+  return hipGetLastError();
+}
+
+}  // namespace tsr

@@ -151,6 +151,20 @@ def test_few_row_items():
     assert make([req(n_rows=9)], model(hq=40), split_tiles=-1, attn_kernel=1).num_attn_items == 2 * 9 * 2
 
 
+def test_many_row_items():
+    # 256 rows x heads an item: 64 rows of 4 heads
+    m = model(hq=8, hkv=2)
+    s = make([req(kv_len=200, n_rows=130)], split_tiles=-1)
+    assert s.attn_item_rows == 256 and s.num_attn_items == 2 * 3
+    # a request with few rows beside it keeps the other kernel's items
+    s = make([req(kv_len=200, n_rows=130), req(kv_len=40, n_rows=1, first=20)], split_tiles=-1)
+    assert s.attn_item_rows == 256 and s.num_attn_items == 2 * 3 + 2
+    assert make([req(kv_len=200, n_rows=2)], m).attn_item_rows == 16
+    assert make([req(kv_len=200, n_rows=2)], m, attn_kernel=2).attn_item_rows == 256
+    refused(P.TSR_ERR_UNSUPPORTED, "bf16 activations only", m=model(kv="f32"), attn_kernel=2)
+    assert make([req(kv_len=200, n_rows=130)], model(kv="f32")).attn_item_rows == 16
+
+
 def test_key_ranges():
     long = [req(kv_len=16 * 1024, page=16)]
     m = model(hq=8, hkv=2)
