@@ -32,6 +32,11 @@ constexpr int kTileBytes = kStepKeys * kRowBytes;
 
 // K buffers; bytes of a wave's own space for a tile; direct loads a wave issues
 // for a tile; 16-byte runs of V a lane converts.
+// Fragments of the second block's queries that stay in LDS: two waves a SIMD
+// leave 256 registers a wave, of which O takes 128, S 32 and the other
+// queries the rest but some 40.
+constexpr int kQInLds = 3;
+
 template <bool F4> struct Staging;
 template <> struct Staging<false> {
   static constexpr int kKBufs = 3, kRaw = 2048, kLoads = 4, kVRuns = 2;
@@ -40,6 +45,10 @@ template <> struct Staging<true> {
   static constexpr int kKBufs = 2, kRaw = 1280, kLoads = 2, kVRuns = 4;
 };
 
+__device__ __forceinline__ uint32_t pack_f16x2(float a, float b) {
+  const f16x2 h = {(_Float16)a, (_Float16)b};
+  return __builtin_bit_cast(uint32_t, h);
+}
 __device__ __forceinline__ uint32_t bf16x2_to_f16x2(uint32_t w) {
   const f16x2 h = {(_Float16)__uint_as_float(w << 16),
                    (_Float16)__uint_as_float(w & 0xffff0000u)};
@@ -55,12 +64,13 @@ __device__ __forceinline__ uint32_t finite_or_0(uint32_t w) {
 }
 
 template <bool F4>
-__global__ __launch_bounds__(64 * kRowWaves, 1) void step_rows_kernel(const StepAttnArgs a) {
+__global__ __launch_bounds__(64 * kRowWaves, 2) void step_rows_kernel(const StepAttnArgs a) {
   using S = Staging<F4>;
   __shared__ __attribute__((aligned(1024))) uint8_t kl[S::kKBufs * kTileBytes];
   __shared__ __attribute__((aligned(1024))) uint8_t vl[2 * kTileBytes];
   __shared__ __attribute__((aligned(1024))) uint8_t raw[kRowWaves * 2 * S::kRaw];
   __shared__ Sight sights[kStepRowVecs];
+  __shared__ __attribute__((aligned(16))) uint4 q_lds[kRowWaves][kQInLds][64];
   __shared__ uint32_t bad_v[kRowWaves];   // wave w replaced values that are not finite
 
   const StepItem it = a.items[blockIdx.x];
@@ -88,14 +98,22 @@ __global__ __launch_bounds__(64 * kRowWaves, 1) void step_rows_kernel(const Step
     page = uniform_i32(bt + (min(tile_key(t) + 16 * sb, last_blk) >> a.log2_page));
   };
   uint8_t* const mine = raw + w * (2 * S::kRaw);
-  const int skey = 8 * half + (lane >> 4);   // bf16 V: this key and the one 4 on
+  // the lane number again, so that nothing derived from it is kept across the
+  // products, whose registers are all taken
+  auto lane_now = [&]() __attribute__((always_inline)) {
+    int x;
+    asm volatile("v_mbcnt_lo_u32_b32 %0, -1, 0\n\tv_mbcnt_hi_u32_b32 %0, -1, %0" : "=&v"(x));
+    return x;
+  };
   auto issue = [&](int t) __attribute__((always_inline)) {
     const int kb = min(tile_key(t) + 16 * sb, last_blk);
     const int top = last - kb;
     const int64_t slot = ((((int64_t)page * a.n_kv_heads + it.kv_head) << a.log2_page) +
                           (kb & page_mask));
     const uint32_t own = lds_addr(mine) + (t & 1) * S::kRaw;
+    const int lane = lane_now(), c16 = lane & 15;
     if constexpr (!F4) {
+      const int skey = 8 * half + (lane >> 4);   // V: this key and the one 4 on
       const uint8_t* kp = static_cast<const uint8_t*>(a.k) + slot * kRowBytes;
       const uint8_t* vp = static_cast<const uint8_t*>(a.v) + slot * kRowBytes;
       const uint32_t dst = lds_addr(kl) + (t % S::kKBufs) * kTileBytes + 4096 * sb + 2048 * half;
@@ -136,8 +154,10 @@ __global__ __launch_bounds__(64 * kRowWaves, 1) void step_rows_kernel(const Step
     const bool masked = key0 < it.full_lo || key0 + kStepKeys - 1 > it.full_hi;
     const uint8_t* own = mine + (t & 1) * S::kRaw;
     uint8_t* vt = vl + (t & 1) * kTileBytes;
+    const int lane = lane_now(), c16 = lane & 15;
     uint4 x[S::kVRuns];
     if constexpr (!F4) {
+      const int skey = 8 * half + (lane >> 4);
 #pragma unroll
       for (int e = 0; e < 2; ++e) {
         const uint4 r = *reinterpret_cast<const uint4*>(own + 1024 * e + 16 * lane);
@@ -189,9 +209,9 @@ __global__ __launch_bounds__(64 * kRowWaves, 1) void step_rows_kernel(const Step
   // ---- this wave's vectors: v = 64 w + 32 b + l32 is row v / heads, head v %
   // heads of the item; vectors past the last repeat the last row
   Frag qf[2][8];
-  // keys [seen_lo, seen_hi] hold all that the wave's rows see beside the sinks
-  // [0, sink_hi); [full_lo, full_hi] is seen by all of them
-  int seen_lo = INT32_MAX, seen_hi = -1, sink_hi = 0, full_lo = 0, full_hi = INT32_MAX;
+  // keys [seen_lo, seen_hi] hold all that the wave's rows see beside the sinks,
+  // which end at sink_hi
+  int seen_lo = INT32_MAX, seen_hi = -1, sink_hi = 0;
 #pragma unroll
   for (int b = 0; b < 2; ++b) {
     const int v = 64 * w + 32 * b + l32;
@@ -215,22 +235,16 @@ __global__ __launch_bounds__(64 * kRowWaves, 1) void step_rows_kernel(const Step
       seen_hi = max(seen_hi, row.pos);
       sink_hi = max(sink_hi, min(sight.shi, sight.wlo));
     }
-    full_lo = max(full_lo, sight.wlo);
-    full_hi = min(full_hi, some ? row.pos : -1);
   }
 #pragma unroll
   for (int o = 1; o < 32; o <<= 1) {
     seen_lo = min(seen_lo, __shfl_xor(seen_lo, o));
     seen_hi = max(seen_hi, __shfl_xor(seen_hi, o));
     sink_hi = max(sink_hi, __shfl_xor(sink_hi, o));
-    full_lo = max(full_lo, __shfl_xor(full_lo, o));
-    full_hi = min(full_hi, __shfl_xor(full_hi, o));
   }
   seen_lo = __builtin_amdgcn_readfirstlane(seen_lo);
   seen_hi = __builtin_amdgcn_readfirstlane(seen_hi);
   sink_hi = __builtin_amdgcn_readfirstlane(sink_hi);
-  full_lo = __builtin_amdgcn_readfirstlane(full_lo);
-  full_hi = __builtin_amdgcn_readfirstlane(full_hi);
   const bool active = 64 * w < it.n_rows * it.n_heads;
 
   f32x16 o[2][4];
@@ -246,7 +260,9 @@ __global__ __launch_bounds__(64 * kRowWaves, 1) void step_rows_kernel(const Step
 #pragma unroll
   for (int b = 0; b < 2; ++b)
 #pragma unroll
-    for (int k = 0; k < 8; ++k) asm volatile("" : "+a"(qf[b][k].b));
+    for (int k = 0; k < 8; ++k) asm volatile("" : "+v"(qf[b][k].b));
+#pragma unroll
+  for (int k = 0; k < kQInLds; ++k) q_lds[w][k][lane] = qf[1][8 - kQInLds + k].u;
   const float sc = a.scale_log2e;
   // operand reads: K fragment k at kfl + (k / 2) 1024 + (k % 2) 512; V^T
   // fragment (16 keys h, 32 dims db) at (vfl ^ 64 db) + 4096 h, + 2048
@@ -261,25 +277,25 @@ __global__ __launch_bounds__(64 * kRowWaves, 1) void step_rows_kernel(const Step
       __attribute__((always_inline)) {
     constexpr bool MASK = decltype(mask_tag)::value;
     f32x16 s[2];
-    f16x8 pf[2][2];
+    uint32_t pw[2][8];   // P as fp16 pairs
     float lt[2];
-    auto scores = [&](int b, const Frag (&kf)[8]) __attribute__((always_inline)) {
-#pragma unroll
-      for (int r = 0; r < 16; ++r) s[b][r] = 0.0f;
-#pragma unroll
-      for (int k = 0; k < 8; ++k)
-        s[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[k].b, qf[b][k].b, s[b], 0, 0, 0);
-    };
     auto probabilities = [&](int b) __attribute__((always_inline)) {
       const float mc = m[b] == -INFINITY ? 0.0f : m[b] * sc;
-      float ls[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+      float ls[2] = {0.0f, 0.0f};
 #pragma unroll
-      for (int r = 0; r < 16; ++r) {
-        const float p = __builtin_amdgcn_exp2f(fmaf(s[b][r], sc, -mc));
-        ls[r & 3] += p;
-        pf[b][r >> 3][r & 7] = (_Float16)p;
+      for (int r = 0; r < 16; r += 4) {
+        float p[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          p[e] = __builtin_amdgcn_exp2f(fmaf(s[b][r + e], sc, -mc));
+          ls[e & 1] += p[e];
+        }
+        pw[b][r / 2] = pack_f16x2(p[0], p[1]);
+        pw[b][r / 2 + 1] = pack_f16x2(p[2], p[3]);
+        // packed now, not after the check below: 16 registers fewer
+        asm volatile("" : "+v"(pw[b][r / 2]), "+v"(pw[b][r / 2 + 1]));
       }
-      lt[b] = (ls[0] + ls[1]) + (ls[2] + ls[3]);
+      lt[b] = ls[0] + ls[1];
     };
     auto softmax = [&](int b) __attribute__((always_inline)) {
       if constexpr (MASK) {
@@ -309,67 +325,82 @@ __global__ __launch_bounds__(64 * kRowWaves, 1) void step_rows_kernel(const Step
         probabilities(b);
       }
       l[b] += lt[b];
+#pragma unroll
+      for (int db = 0; db < 4; ++db) asm volatile("" : "+v"(o[b][db]));
     };
-    Frag vf[2][4];
-    auto outputs = [&](int b) __attribute__((always_inline)) {
 #pragma unroll
-      for (int h = 0; h < 2; ++h)
+    for (int b = 0; b < 2; ++b)
 #pragma unroll
-        for (int db = 0; db < 4; ++db)
-          o[b][db] = __builtin_amdgcn_mfma_f32_32x32x16_f16(vf[h][db].h, pf[b][h], o[b][db], 0, 0, 0);
-    };
-    {
-      Frag kf[8];
+      for (int r = 0; r < 16; ++r) s[b][r] = 0.0f;
 #pragma unroll
-      for (int k = 0; k < 8; ++k)
-        kf[k].u = *reinterpret_cast<const uint4*>(kt + kfl + 1024 * (k >> 1) + 512 * (k & 1));
-      scores(0, kf);
-      scores(1, kf);
+    for (int k = 0; k < 8; ++k) {
+      Frag f;
+      f.u = *reinterpret_cast<const uint4*>(kt + kfl + 1024 * (k >> 1) + 512 * (k & 1));
+      s[0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f.b, qf[0][k].b, s[0], 0, 0, 0);
+      Frag q1 = qf[1][k];
+      if (k >= 8 - kQInLds) q1.u = q_lds[w][k - 8 + kQInLds][lane];
+      s[1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f.b, q1.b, s[1], 0, 0, 0);
     }
     softmax(0);
     settle(0);
+    softmax(1);
+    settle(1);
+    Frag pf[2][2];
+#pragma unroll
+    for (int b = 0; b < 2; ++b)
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+        pf[b][h].u = make_uint4(pw[b][4 * h], pw[b][4 * h + 1], pw[b][4 * h + 2], pw[b][4 * h + 3]);
     const uint32_t va = lds_addr(vt) + vfl;
 #pragma unroll
     for (int h = 0; h < 2; ++h)
 #pragma unroll
       for (int db = 0; db < 4; ++db) {
+        Frag f;
         const uint2 x = lds_read_transposed((va ^ (64 * db)) + 4096 * h);
         const uint2 y = lds_read_transposed((va ^ (64 * db)) + 4096 * h + 2048);
-        vf[h][db].u = make_uint4(x.x, x.y, y.x, y.y);
+        f.u = make_uint4(x.x, x.y, y.x, y.y);
+#pragma unroll
+        for (int b = 0; b < 2; ++b)
+          o[b][db] = __builtin_amdgcn_mfma_f32_32x32x16_f16(f.h, pf[b][h].h, o[b][db], 0, 0, 0);
       }
-    outputs(0);
-    softmax(1);
-    settle(1);
-    outputs(1);
   };
 
   // (the queries' wait above was for the first tiles too)
   if (nt > 0) convert(0);
   __syncthreads();
-  for (int t = 0; t < nt; ++t) {
-    if (t + 2 < nt) {
-      wait_lds();   // the space it goes to has been read
-      issue(t + 2);
-      if (t + 3 < nt) fetch_page(t + 3);
+  auto run = [&](int t0, int t1, auto mask_tag) __attribute__((always_inline)) {
+    for (int t = t0; t < t1; ++t) {
+      if (t + 2 < nt) {
+        wait_lds();   // the space it goes to has been read
+        issue(t + 2);
+        if (t + 3 < nt) fetch_page(t + 3);
+      }
+      const int key0 = tile_key(t);
+      const uint8_t* kt = kl + (t % S::kKBufs) * kTileBytes;
+      const uint8_t* vt = vl + (t & 1) * kTileBytes;
+      if constexpr (decltype(mask_tag)::value) {
+        if (active && ((key0 <= seen_hi && key0 + kStepKeys > seen_lo) || key0 < sink_hi))
+          tile(key0, mask_tag, kt, vt);
+      } else {
+        tile(key0, mask_tag, kt, vt);
+      }
+      if (t + 1 < nt) {
+        if (t + 2 < nt)
+          wait_vm<S::kLoads>();
+        else
+          wait_vm<0>();
+        convert(t + 1);
+      }
+      __syncthreads();
     }
-    const int key0 = tile_key(t);
-    const uint8_t* kt = kl + (t % S::kKBufs) * kTileBytes;
-    const uint8_t* vt = vl + (t & 1) * kTileBytes;
-    if (active && ((key0 <= seen_hi && key0 + kStepKeys > seen_lo) || key0 < sink_hi)) {
-      if (key0 < full_lo || key0 + kStepKeys - 1 > full_hi)
-        tile(key0, std::true_type{}, kt, vt);
-      else
-        tile(key0, std::false_type{}, kt, vt);
-    }
-    if (t + 1 < nt) {
-      if (t + 2 < nt)
-        wait_vm<S::kLoads>();
-      else
-        wait_vm<0>();
-      convert(t + 1);
-    }
-    __syncthreads();
-  }
+  };
+  // tiles [f0, f1) are seen in full by every row of the item
+  const int f0 = min(nt, na + max(0, (it.full_lo + kStepKeys - 1) / kStepKeys - it.b0));
+  const int f1 = max(f0, min(nt, na + (it.full_hi + 1) / kStepKeys - it.b0));
+  run(0, f0, std::true_type{});
+  run(f0, f1, std::false_type{});
+  run(f1, nt, std::true_type{});
 
   if (!active) return;
   // ---- values that are not finite, for the rows that see them
