@@ -29,21 +29,13 @@ namespace {
 constexpr int kRowWaves = 4;
 constexpr int kRowBytes = 2 * kD;   // a key's K or V row in LDS
 constexpr int kTileBytes = kStepKeys * kRowBytes;
+constexpr int kPairBytes = 2 * kTileBytes;
+constexpr int kBlkBytes = 16 * kRowBytes;   // a 16-key block of either
 
-// K buffers; bytes of a wave's own space for a tile; direct loads a wave issues
-// for a tile; 16-byte runs of V a lane converts.
 // Fragments of the second block's queries that stay in LDS: two waves a SIMD
 // leave 256 registers a wave, of which O takes 128, S 32 and the other
 // queries the rest but some 40.
-constexpr int kQInLds = 3;
-
-template <bool F4> struct Staging;
-template <> struct Staging<false> {
-  static constexpr int kKBufs = 3, kRaw = 2048, kLoads = 4, kVRuns = 2;
-};
-template <> struct Staging<true> {
-  static constexpr int kKBufs = 2, kRaw = 1280, kLoads = 2, kVRuns = 4;
-};
+constexpr int kQInLds = 2;
 
 __device__ __forceinline__ uint32_t pack_f16x2(float a, float b) {
   const f16x2 h = {(_Float16)a, (_Float16)b};
@@ -65,10 +57,9 @@ __device__ __forceinline__ uint32_t finite_or_0(uint32_t w) {
 
 template <bool F4>
 __global__ __launch_bounds__(64 * kRowWaves, 2) void step_rows_kernel(const StepAttnArgs a) {
-  using S = Staging<F4>;
-  __shared__ __attribute__((aligned(1024))) uint8_t kl[S::kKBufs * kTileBytes];
-  __shared__ __attribute__((aligned(1024))) uint8_t vl[2 * kTileBytes];
-  __shared__ __attribute__((aligned(1024))) uint8_t raw[kRowWaves * 2 * S::kRaw];
+  // two pairs of tiles, K and V
+  __shared__ __attribute__((aligned(1024))) uint8_t kl[2 * kPairBytes];
+  __shared__ __attribute__((aligned(1024))) uint8_t vl[2 * kPairBytes];
   __shared__ Sight sights[kStepRowVecs];
   __shared__ __attribute__((aligned(16))) uint4 q_lds[kRowWaves][kQInLds][64];
   __shared__ uint32_t bad_v[kRowWaves];   // wave w replaced values that are not finite
@@ -86,123 +77,115 @@ __global__ __launch_bounds__(64 * kRowWaves, 2) void step_rows_kernel(const Step
   auto tile_key = [&](int t) { return kStepKeys * (t < na ? it.a0 + t : it.b0 + t - na); };
   const int last = it.kv_len - 1, last_blk = last & ~15;
 
-  // ---- staging, two tiles ahead.  Wave w serves 16-key block w / 2 of a tile:
-  //   bf16   K's 32-dim runs 2 (w % 2) .. + 1, by direct loads into place, and
-  //          V's keys 8 (w % 2) .. + 7, by direct loads into the wave's own
-  //          space, from where they go on as fp16 rows a tile later;
-  //   4-bit  K (w even) or V (odd): codes and scales into the wave's own space.
+  // ---- staging, a pair of tiles ahead: wave w brings 16-key block w of the
+  // pair, K and V, by direct loads.
+  //   bf16   K in operand order; V as rows with their chunks permuted, which
+  //          its wave turns into fp16 in place once they are there;
+  //   4-bit  codes and scales to the front of the block's space in either
+  //          buffer, from where its wave spreads them over it.
   // Keys past the last one read it again (as in step_attn.hip).
-  const int sb = w >> 1, half = w & 1;
-  int page = 0;
-  auto fetch_page = [&](int t) {
-    page = uniform_i32(bt + (min(tile_key(t) + 16 * sb, last_blk) >> a.log2_page));
-  };
-  uint8_t* const mine = raw + w * (2 * S::kRaw);
-  // the lane number again, so that nothing derived from it is kept across the
-  // products, whose registers are all taken
+  // The lane number is taken anew, so that nothing derived from it is kept
+  // across the products, whose registers are all taken.
   auto lane_now = [&]() __attribute__((always_inline)) {
     int x;
     asm volatile("v_mbcnt_lo_u32_b32 %0, -1, 0\n\tv_mbcnt_hi_u32_b32 %0, -1, %0" : "=&v"(x));
     return x;
   };
-  auto issue = [&](int t) __attribute__((always_inline)) {
-    const int kb = min(tile_key(t) + 16 * sb, last_blk);
-    const int top = last - kb;
-    const int64_t slot = ((((int64_t)page * a.n_kv_heads + it.kv_head) << a.log2_page) +
-                          (kb & page_mask));
-    const uint32_t own = lds_addr(mine) + (t & 1) * S::kRaw;
-    const int lane = lane_now(), c16 = lane & 15;
+  auto my_key = [&](int t) {
+    return min(tile_key(min(t + (w >> 1), nt - 1)) + 16 * (w & 1), last_blk);
+  };
+  int page = 0;
+  auto fetch_page = [&](int t) { page = uniform_i32(bt + (my_key(t) >> a.log2_page)); };
+  const uint32_t page_keys = (uint32_t)a.n_kv_heads << a.log2_page;   // of all heads
+  const uint32_t head_key = (uint32_t)it.kv_head << a.log2_page;
+  auto issue = [&](int t, int slot) __attribute__((always_inline)) {
+    const int kb = my_key(t), top = last - kb;
+    const uint64_t key = (uint64_t)(uint32_t)page * page_keys + head_key + (kb & page_mask);
+    const uint32_t kd = lds_addr(kl) + slot * kPairBytes + w * kBlkBytes;
+    const uint32_t vd = lds_addr(vl) + slot * kPairBytes + w * kBlkBytes;
+    const int lane = lane_now(), c16 = lane & 15, c4 = lane >> 4;
+    const int kk = min(c16, top);
     if constexpr (!F4) {
-      const int skey = 8 * half + (lane >> 4);   // V: this key and the one 4 on
-      const uint8_t* kp = static_cast<const uint8_t*>(a.k) + slot * kRowBytes;
-      const uint8_t* vp = static_cast<const uint8_t*>(a.v) + slot * kRowBytes;
-      const uint32_t dst = lds_addr(kl) + (t % S::kKBufs) * kTileBytes + 4096 * sb + 2048 * half;
-      const uint32_t ko = min(c16, top) * kRowBytes + 128 * half + 16 * (lane >> 4);
-      dma16(kp, ko, dst);
-      dma16(kp, ko + 64, dst + 1024);
-      dma16(vp, min(skey, top) * kRowBytes + 16 * c16, own);
-      dma16(vp, min(skey + 4, top) * kRowBytes + 16 * c16, own + 1024);
+      const uint8_t* kp = static_cast<const uint8_t*>(a.k) + key * kRowBytes;
+      const uint8_t* vp = static_cast<const uint8_t*>(a.v) + key * kRowBytes;
+      const uint32_t ko = kk * kRowBytes + 16 * c4;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) dma16(kp, ko + 64 * e, kd + 1024 * e);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const int k = 4 * e + c4;
+        dma16(vp, min(k, top) * kRowBytes + 16 * (c16 ^ (2 * (k & 7))), vd + 1024 * e);
+      }
     } else {
-      const uint8_t* cp = static_cast<const uint8_t*>(half ? a.v : a.k) + slot * (kD / 2);
-      const int64_t ss = ((((int64_t)page * 2 + half) * a.n_kv_heads + it.kv_head)
-                          << a.log2_page) + (kb & page_mask);
-      const int kk = min(c16, top);
-      dma16(cp, kk * (kD / 2) + 16 * (lane >> 4), own);
-      dma4(a.scales + ss * (kD / kScaleDims), kk * (kD / kScaleDims), own + 1024);
+      const uint8_t* kp = static_cast<const uint8_t*>(a.k) + key * (kD / 2);
+      const uint8_t* vp = static_cast<const uint8_t*>(a.v) + key * (kD / 2);
+      const uint8_t* sp = a.scales + (key + (uint64_t)(uint32_t)page * page_keys) *
+                                         (kD / kScaleDims);
+      dma16(kp, kk * (kD / 2) + 16 * c4, kd);
+      dma16(vp, kk * (kD / 2) + 16 * c4, vd);
+      dma4(sp, kk * (kD / kScaleDims), kd + 1024);
+      dma4(sp, (kk + page_keys) * (kD / kScaleDims), vd + 1024);
     }
   };
   // fp16 values of V in tiles that not every row sees in full: a masked key
   // weighs 0, but 0 x inf is not 0, so values that are not finite are 0 there,
   // and the rows that see them get them at the end
-  auto clean = [&](uint4 (&x)[S::kVRuns]) __attribute__((always_inline)) {
+  auto clean = [&](uint4 (&x)[4]) __attribute__((always_inline)) {
     uint32_t off = 0;
 #pragma unroll
-    for (int e = 0; e < S::kVRuns; ++e)
+    for (int e = 0; e < 4; ++e)
       off |= f16x2_not_finite(x[e].x) | f16x2_not_finite(x[e].y) | f16x2_not_finite(x[e].z) |
              f16x2_not_finite(x[e].w);
     if (__builtin_amdgcn_ballot_w64(off != 0)) {
-      if (lane == 0) bad_v[w] = 1;
+      if (lane_now() == 0) bad_v[w] = 1;
 #pragma unroll
-      for (int e = 0; e < S::kVRuns; ++e)
+      for (int e = 0; e < 4; ++e)
         x[e] = make_uint4(finite_or_0(x[e].x), finite_or_0(x[e].y), finite_or_0(x[e].z),
                           finite_or_0(x[e].w));
     }
   };
-  // the wave's part of tile t, from its own space on
-  auto convert = [&](int t) __attribute__((always_inline)) {
-    const int key0 = tile_key(t);
+  // what the wave's loads brought, into the form the products take
+  auto convert = [&](int t, int slot) __attribute__((always_inline)) {
+    const int key0 = tile_key(min(t + (w >> 1), nt - 1));
     const bool masked = key0 < it.full_lo || key0 + kStepKeys - 1 > it.full_hi;
-    const uint8_t* own = mine + (t & 1) * S::kRaw;
-    uint8_t* vt = vl + (t & 1) * kTileBytes;
-    const int lane = lane_now(), c16 = lane & 15;
-    uint4 x[S::kVRuns];
+    uint8_t* kt = kl + slot * kPairBytes + w * kBlkBytes;
+    uint8_t* vt = vl + slot * kPairBytes + w * kBlkBytes;
+    const int lane = lane_now(), c16 = lane & 15, c4 = lane >> 4;
+    uint4 x[4];
     if constexpr (!F4) {
-      const int skey = 8 * half + (lane >> 4);
 #pragma unroll
-      for (int e = 0; e < 2; ++e) {
-        const uint4 r = *reinterpret_cast<const uint4*>(own + 1024 * e + 16 * lane);
-        x[e] = make_uint4(bf16x2_to_f16x2(r.x), bf16x2_to_f16x2(r.y), bf16x2_to_f16x2(r.z),
-                          bf16x2_to_f16x2(r.w));
-      }
-      if (masked) clean(x);
-#pragma unroll
-      for (int e = 0; e < 2; ++e) {
-        const int key = 16 * sb + skey + 4 * e;
-        *reinterpret_cast<uint4*>(vt + key * kRowBytes + 16 * (c16 ^ (2 * (key & 7)))) = x[e];
-      }
+      for (int e = 0; e < 4; ++e) x[e] = *reinterpret_cast<const uint4*>(vt + 1024 * e + 16 * lane);
     } else {
-      // this lane's key c16 and 32 dims
-      const uint4 r = *reinterpret_cast<const uint4*>(own + 16 * lane);
-      const float f = e2m1_factor(own[1024 + 4 * c16 + (lane >> 4)]);
-      const uint32_t c[4] = {r.x, r.y, r.z, r.w};
+      // this lane's key c16 and 32 dims of each
+      const uint4 kr = *reinterpret_cast<const uint4*>(kt + 16 * lane);
+      const uint4 vr = *reinterpret_cast<const uint4*>(vt + 16 * lane);
+      const float kf = e2m1_factor(kt[1024 + 4 * c16 + c4]);
+      const float vf = e2m1_factor(vt[1024 + 4 * c16 + c4]);
+      const uint32_t kc[4] = {kr.x, kr.y, kr.z, kr.w}, vc[4] = {vr.x, vr.y, vr.z, vr.w};
+      wait_lds();   // all of the wave's codes are read before they are written over
 #pragma unroll
-      for (int e = 0; e < 4; ++e) x[e] = e2m1_decode8(c[e], f);
-      if (!half) {
-        uint8_t* kt = kl + (t % S::kKBufs) * kTileBytes + 4096 * sb + 1024 * (lane >> 4);
+      for (int e = 0; e < 4; ++e)
+        *reinterpret_cast<uint4*>(kt + 1024 * c4 + 256 * e + 16 * c16) = e2m1_decode8(kc[e], kf);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) *reinterpret_cast<uint4*>(kt + 256 * e + 16 * c16) = x[e];
-      } else {
+      for (int e = 0; e < 4; ++e) x[e] = e2m1_decode8(vc[e], vf);
+    }
 #pragma unroll
-        for (int e = 0; e < 4; ++e)
-          x[e] = make_uint4(bf16x2_to_f16x2(x[e].x), bf16x2_to_f16x2(x[e].y),
-                            bf16x2_to_f16x2(x[e].z), bf16x2_to_f16x2(x[e].w));
-        if (masked) clean(x);
+    for (int e = 0; e < 4; ++e)
+      x[e] = make_uint4(bf16x2_to_f16x2(x[e].x), bf16x2_to_f16x2(x[e].y),
+                        bf16x2_to_f16x2(x[e].z), bf16x2_to_f16x2(x[e].w));
+    if (masked) clean(x);
 #pragma unroll
-        for (int e = 0; e < 4; ++e)
-          *reinterpret_cast<uint4*>(vt + (16 * sb + c16) * kRowBytes +
-                                    16 * ((4 * (lane >> 4) + e) ^ (2 * (c16 & 7)))) = x[e];
-      }
+    for (int e = 0; e < 4; ++e) {
+      uint8_t* to = F4 ? vt + c16 * kRowBytes + 16 * ((4 * c4 + e) ^ (2 * (c16 & 7)))
+                       : vt + 1024 * e + 16 * lane;
+      *reinterpret_cast<uint4*>(to) = x[e];
     }
   };
 
   if (tid < kRowWaves) bad_v[tid] = 0;
   if (nt > 0) {
     fetch_page(0);
-    issue(0);
-  }
-  if (nt > 1) {
-    fetch_page(1);
-    issue(1);
+    issue(0, 0);
   }
   if (nt > 2) fetch_page(2);
 
@@ -332,6 +315,7 @@ __global__ __launch_bounds__(64 * kRowWaves, 2) void step_rows_kernel(const Step
     for (int b = 0; b < 2; ++b)
 #pragma unroll
       for (int r = 0; r < 16; ++r) s[b][r] = 0.0f;
+    __builtin_amdgcn_s_setprio(1);
 #pragma unroll
     for (int k = 0; k < 8; ++k) {
       Frag f;
@@ -341,6 +325,16 @@ __global__ __launch_bounds__(64 * kRowWaves, 2) void step_rows_kernel(const Step
       if (k >= 8 - kQInLds) q1.u = q_lds[w][k - 8 + kQInLds][lane];
       s[1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f.b, q1.b, s[1], 0, 0, 0);
     }
+    __builtin_amdgcn_s_setprio(0);
+    // keep LDS reads in flight ahead of the products (scheduling groups: 0x100
+    // LDS read, 0x008 matrix)
+    __builtin_amdgcn_sched_group_barrier(0x100, 5, 0);
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      __builtin_amdgcn_sched_group_barrier(0x008, 2, 0);
+      __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+    }
+    __builtin_amdgcn_sched_barrier(0);
     softmax(0);
     settle(0);
     softmax(1);
@@ -364,33 +358,42 @@ __global__ __launch_bounds__(64 * kRowWaves, 2) void step_rows_kernel(const Step
         for (int b = 0; b < 2; ++b)
           o[b][db] = __builtin_amdgcn_mfma_f32_32x32x16_f16(f.h, pf[b][h].h, o[b][db], 0, 0, 0);
       }
+    __builtin_amdgcn_sched_group_barrier(0x100, 6, 0);
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      __builtin_amdgcn_sched_group_barrier(0x008, 2, 0);
+      __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
+    }
   };
 
-  // (the queries' wait above was for the first tiles too)
-  if (nt > 0) convert(0);
+  __syncthreads();   // bad_v is clear
+  // (the queries' wait above was for the first pair too)
+  if (nt > 0) convert(0, 0);
   __syncthreads();
-  auto run = [&](int t0, int t1, auto mask_tag) __attribute__((always_inline)) {
-    for (int t = t0; t < t1; ++t) {
+  auto run = [&](int p0, int p1, auto mask_tag) __attribute__((always_inline)) {
+    for (int p = p0; p < p1; ++p) {
+      const int t = 2 * p, slot = p & 1;
       if (t + 2 < nt) {
-        wait_lds();   // the space it goes to has been read
-        issue(t + 2);
-        if (t + 3 < nt) fetch_page(t + 3);
+        wait_lds();   // the pair before last has been read
+        issue(t + 2, slot ^ 1);
+        if (t + 4 < nt) fetch_page(t + 4);
       }
-      const int key0 = tile_key(t);
-      const uint8_t* kt = kl + (t % S::kKBufs) * kTileBytes;
-      const uint8_t* vt = vl + (t & 1) * kTileBytes;
-      if constexpr (decltype(mask_tag)::value) {
-        if (active && ((key0 <= seen_hi && key0 + kStepKeys > seen_lo) || key0 < sink_hi))
-          tile(key0, mask_tag, kt, vt);
-      } else {
-        tile(key0, mask_tag, kt, vt);
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        const uint8_t* kt = kl + slot * kPairBytes + e * kTileBytes;
+        const uint8_t* vt = vl + slot * kPairBytes + e * kTileBytes;
+        if constexpr (decltype(mask_tag)::value) {
+          if (t + e >= nt) break;
+          const int key0 = tile_key(t + e);
+          if (active && ((key0 <= seen_hi && key0 + kStepKeys > seen_lo) || key0 < sink_hi))
+            tile(key0, mask_tag, kt, vt);
+        } else {
+          tile(0, mask_tag, kt, vt);
+        }
       }
-      if (t + 1 < nt) {
-        if (t + 2 < nt)
-          wait_vm<S::kLoads>();
-        else
-          wait_vm<0>();
-        convert(t + 1);
+      if (t + 2 < nt) {
+        wait_vm<0>();
+        convert(t + 2, slot ^ 1);
       }
       __syncthreads();
     }
@@ -398,9 +401,10 @@ __global__ __launch_bounds__(64 * kRowWaves, 2) void step_rows_kernel(const Step
   // tiles [f0, f1) are seen in full by every row of the item
   const int f0 = min(nt, na + max(0, (it.full_lo + kStepKeys - 1) / kStepKeys - it.b0));
   const int f1 = max(f0, min(nt, na + (it.full_hi + 1) / kStepKeys - it.b0));
-  run(0, f0, std::true_type{});
-  run(f0, f1, std::false_type{});
-  run(f1, nt, std::true_type{});
+  const int n_pairs = (nt + 1) / 2, p0 = min(n_pairs, (f0 + 1) / 2), p1 = max(p0, f1 / 2);
+  run(0, p0, std::true_type{});
+  run(p0, p1, std::false_type{});
+  run(p1, n_pairs, std::true_type{});
 
   if (!active) return;
   // ---- values that are not finite, for the rows that see them
