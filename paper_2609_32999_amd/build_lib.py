@@ -27,7 +27,7 @@ COMMON = [
 ]
 # step_rows.hip keeps 246 vector and 64 accumulation registers a wave: its
 # products have to deliver into the former
-EXTRA = {"step_rows.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"]}
+EXTRA = {f: ["-mllvm", "-amdgpu-mfma-vgpr-form"] for f in ("step_attn.hip", "step_rows.hip")}
 
 
 def _hipcc() -> str:

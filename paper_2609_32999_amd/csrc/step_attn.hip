@@ -45,12 +45,12 @@ template <> struct Tile<false> {
   static constexpr int kStages = 2, kBytes = 16384, kLoads = 16, kRows = 0;
 };
 template <> struct Tile<true> {
-  static constexpr int kStages = 4, kBytes = 4608, kLoads = 6, kRows = 8192;
+  static constexpr int kStages = 2, kBytes = 4608, kLoads = 6, kRows = 4096;
 };
 constexpr int kStepWaves = 4;
 
 template <bool F4>
-__global__ __launch_bounds__(64 * kStepWaves) void step_attn_kernel(const StepAttnArgs a) {
+__global__ __launch_bounds__(64 * kStepWaves, F4 ? 3 : 1) void step_attn_kernel(const StepAttnArgs a) {
   using T = Tile<F4>;
   constexpr int NW = kStepWaves, ST = T::kStages;
   constexpr int kWaveLds = ST * T::kBytes + T::kRows;
@@ -163,45 +163,44 @@ __global__ __launch_bounds__(64 * kStepWaves) void step_attn_kernel(const StepAt
   const int tkey = 4 * c4 + (c16 >> 2);
   const uint32_t toff = tkey * (2 * kD) + 32 * (tkey & 7) + 8 * (c16 & 3);
 
+  // 4-bit: 16 keys' V as bf16 rows in the wave's own space, from the lane's key
+  // and 32 dims.  (LDS keeps a wave's accesses in order; the fences keep the
+  // compiler to it.)
+  auto put_v_rows = [&](const uint8_t* t, int b) __attribute__((always_inline)) {
+    const uint4 c = *reinterpret_cast<const uint4*>(t + 2048 + 1024 * b + 16 * lane);
+    const float vf = e2m1_factor(t[4096 + 256 * b + 64 + 4 * c16 + c4]);
+    const uint32_t w4[4] = {c.x, c.y, c.z, c.w};
+    uint8_t* rows = mine + ST * T::kBytes;
+    asm volatile("" ::: "memory");
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+      *reinterpret_cast<uint4*>(rows + c16 * (2 * kD) + 16 * ((4 * c4 + k) ^ (2 * (c16 & 7)))) =
+          e2m1_decode8(w4[k], vf);
+    asm volatile("" ::: "memory");
+  };
+
   auto tile = [&](int key0, const uint8_t* t) __attribute__((always_inline)) {
     // ---- scores
     f32x4 s[2];
-    uint8_t* vrows;
-    if constexpr (!F4) {
-      vrows = const_cast<uint8_t*>(t) + 8192;
 #pragma unroll
-      for (int b = 0; b < 2; ++b) {
-        s[b] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-          Frag f;
-          f.u = *reinterpret_cast<const uint4*>(t + 4096 * b + 1024 * k + 16 * lane);
-          s[b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f.b, qf[k].b, s[b], 0, 0, 0);
-        }
-      }
-    } else {
-      vrows = mine + ST * T::kBytes;
-#pragma unroll
-      for (int b = 0; b < 2; ++b) {
-        const uint4 kc = *reinterpret_cast<const uint4*>(t + 1024 * b + 16 * lane);
-        const uint4 vc = *reinterpret_cast<const uint4*>(t + 2048 + 1024 * b + 16 * lane);
-        const uint8_t* sp = t + 4096 + 256 * b + 4 * c16 + c4;
-        const float kf = e2m1_factor(sp[0]), vf = e2m1_factor(sp[64]);
-        const uint32_t kw[4] = {kc.x, kc.y, kc.z, kc.w}, vw[4] = {vc.x, vc.y, vc.z, vc.w};
-        s[b] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-          Frag f;
-          f.u = e2m1_decode8(kw[k], kf);
-          s[b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f.b, qf[k].b, s[b], 0, 0, 0);
-        }
-        // V to bf16 rows: the lane's key and 32 dims
+    for (int b = 0; b < 2; ++b) {
+      s[b] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+      Frag f[4];
+      if constexpr (!F4) {
 #pragma unroll
         for (int k = 0; k < 4; ++k)
-          *reinterpret_cast<uint4*>(vrows + (16 * b + c16) * (2 * kD) +
-                                    16 * ((4 * c4 + k) ^ (2 * (c16 & 7)))) =
-              e2m1_decode8(vw[k], vf);
+          f[k].u = *reinterpret_cast<const uint4*>(t + 4096 * b + 1024 * k + 16 * lane);
+      } else {
+        const uint4 c = *reinterpret_cast<const uint4*>(t + 1024 * b + 16 * lane);
+        const float kf = e2m1_factor(t[4096 + 256 * b + 4 * c16 + c4]);
+        f[0].u = e2m1_decode8(c.x, kf);
+        f[1].u = e2m1_decode8(c.y, kf);
+        f[2].u = e2m1_decode8(c.z, kf);
+        f[3].u = e2m1_decode8(c.w, kf);
       }
+#pragma unroll
+      for (int k = 0; k < 4; ++k)
+        s[b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f[k].b, qf[k].b, s[b], 0, 0, 0);
     }
     const bool masked = key0 < it.full_lo || key0 + kStepKeys - 1 > it.full_hi;
     if (masked) {
@@ -247,18 +246,19 @@ __global__ __launch_bounds__(64 * kStepWaves) void step_attn_kernel(const StepAt
       pl[r] = (__bf16)(p[r] - (float)ph[r]);
     }
     // ---- O^T += V^T P^T
-    const uint32_t va = lds_addr(vrows) + toff;
     Frag vf[8];
-    // (LDS keeps a wave's accesses in order; this keeps the compiler to it)
-    if constexpr (F4) asm volatile("" ::: "memory");
 #pragma unroll
-    for (int db = 0; db < 8; ++db)
+    for (int b = 0; b < 2; ++b) {
+      const uint8_t* rows = F4 ? mine + ST * T::kBytes : t + 8192 + 4096 * b;
+      if constexpr (F4) put_v_rows(t, b);
+      const uint32_t va = lds_addr(rows) + toff;
 #pragma unroll
-      for (int b = 0; b < 2; ++b) {
-        const uint2 u = lds_read_transposed((va ^ (32 * db)) + 4096 * b);
+      for (int db = 0; db < 8; ++db) {
+        const uint2 u = lds_read_transposed(va ^ (32 * db));
         vf[db].w[2 * b] = u.x;
         vf[db].w[2 * b + 1] = u.y;
       }
+    }
     // A masked key weighs 0, but 0 x inf is not 0: where a masked tile's V is
     // not finite everywhere, each vector adds the keys it sees one by one.
     bool plain = true;
@@ -287,11 +287,13 @@ __global__ __launch_bounds__(64 * kStepWaves) void step_attn_kernel(const StepAt
         for (int r = 0; r < 8; ++r)
           if (r == 4 * (j >> 4) + (j & 3)) pj = p[r];
         pj = __shfl(pj, 16 * ((j >> 2) & 3) + c16);
+        const uint8_t* rows = F4 ? mine + ST * T::kBytes : t + 8192 + 4096 * (j >> 4);
+        if (F4 && (j & 15) == 0) put_v_rows(t, j >> 4);
         if (!sees(sight, key0 + j)) continue;
 #pragma unroll
         for (int db = 0; db < 8; ++db) {
           const uint2 u = *reinterpret_cast<const uint2*>(
-              vrows + j * (2 * kD) + 32 * (db ^ (j & 7)) + 8 * c4);
+              rows + (j & 15) * (2 * kD) + 32 * (db ^ (j & 7)) + 8 * c4);
           o[db][0] = fmaf(pj, bf16_to_f32(u.x & 0xffffu), o[db][0]);
           o[db][1] = fmaf(pj, bf16_to_f32(u.x >> 16), o[db][1]);
           o[db][2] = fmaf(pj, bf16_to_f32(u.y & 0xffffu), o[db][2]);

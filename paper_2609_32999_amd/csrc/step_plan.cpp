@@ -26,7 +26,7 @@ tsr_status fail_req(tsr_status st, int r, const std::string& msg) {
 
 // A launch for few rows is cut into about this many items a compute unit, of
 // kMinRangeTiles tiles at least; one for many rows into one a unit.
-constexpr int kRangesPerCu = 2;
+constexpr int kRangesPerCu = 3;
 constexpr int kMinRangeTiles = 8;
 constexpr int kMinRowRangeTiles = 16;
 constexpr int64_t kMaxSplitVecs = (int64_t)1 << 21;
