@@ -129,7 +129,12 @@ __global__ __launch_bounds__(64 * kStepWaves, F4 ? 3 : 1) void step_attn_kernel(
 #pragma unroll
   for (int i = 0; i < ST - 1; ++i)
     if (i < n) {
-      fetch_pages(i);
+      if (i == 0) {
+        pg[0] = a.items[blockIdx.x].pg[2 * w];
+        pg[1] = a.items[blockIdx.x].pg[2 * w + 1];
+      } else {
+        fetch_pages(i);
+      }
       issue(i, i);
     }
   if (ST - 1 < n) fetch_pages(ST - 1);
@@ -544,8 +549,10 @@ __global__ __launch_bounds__(64 * kStepWaves) void step_attn_f32_kernel(const St
 
 // ------------------------------------------------------------ key ranges
 // lse = log sum_c exp(lse_c), o = sum_c exp(lse_c - lse) o_c over an item's
-// ranges c, in their order.  Half a wave takes a vector, D / 32 dims a lane;
-// lane c % 32 holds the weight of range c.
+// ranges c, always summed in the same order.  Half a wave reads a partial row,
+// D / 32 dims a lane.  With few ranges a half-wave takes a vector; with many
+// (one long request: 92 ranges took 26 us so) a workgroup does, its eight
+// half-waves every eighth range each.
 struct MergeArgs {
   const StepRow* rows;
   const StepMerge* merges;
@@ -554,28 +561,32 @@ struct MergeArgs {
   float* lse;
   int32_t n_q_heads;
 };
-constexpr int kMergeVecs = 8;   // of a workgroup of 256
-constexpr int kMergeAhead = 8;
+constexpr int kMergeHalves = 8;   // half-waves of a workgroup
+constexpr int kMergeAhead = 8;    // partial rows asked for at once
 
-template <typename E, int D>
-__global__ __launch_bounds__(256) void step_merge_kernel(const MergeArgs a) {
+template <typename E, int D, bool MANY>
+__global__ __launch_bounds__(32 * kMergeHalves) void step_merge_kernel(const MergeArgs a) {
   constexpr int W = D / 32;
   typedef float vec_t __attribute__((ext_vector_type(W)));
   const StepMerge g = a.merges[blockIdx.x];
-  const int lane = threadIdx.x & 31;
-  const int v = blockIdx.y * kMergeVecs + (threadIdx.x >> 5);
+  const int lane = threadIdx.x & 31, half = threadIdx.x >> 5;
+  const int v = MANY ? blockIdx.y : blockIdx.y * kMergeHalves + half;
   const int r = (g.vec0 + v) / g.n_heads, h = g.vec0 + v - r * g.n_heads;
-  if (r >= g.n_rows) return;
+  if (r >= g.n_rows) return;   // (MANY: the whole workgroup)
+  constexpr int STEP = MANY ? kMergeHalves : 1;
+  const int c0 = MANY ? half : 0;
   auto at = [&](int c) { return (int64_t)g.slot0 + (int64_t)c * g.stride + v; };
   auto part = [&](int c) {
     return *reinterpret_cast<const vec_t*>(a.split_o + at(c) * D + W * lane);
   };
   auto range_lse = [&](int c) { return c < g.n_slots ? a.split_lse[at(c)] : -INFINITY; };
+  // this half-wave's ranges: c0 + STEP i
+  const int n = (g.n_slots - c0 + STEP - 1) / STEP;
   const float l0 = range_lse(lane);
   const StepRow row = a.rows[g.row0 + r];
-  vec_t ahead[kMergeAhead];   // past the last range: it again, unused
+  vec_t ahead[kMergeAhead];   // past the last range: range c0 again, unused
 #pragma unroll
-  for (int c = 0; c < kMergeAhead; ++c) ahead[c] = part(min(c, g.n_slots - 1));
+  for (int i = 0; i < kMergeAhead; ++i) ahead[i] = part(i < n ? c0 + STEP * i : min(c0, g.n_slots - 1));
   float mx = l0;
   for (int c = lane + 32; c < g.n_slots; c += 32) mx = fmaxf(mx, range_lse(c));
 #pragma unroll
@@ -585,16 +596,33 @@ __global__ __launch_bounds__(256) void step_merge_kernel(const MergeArgs a) {
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) den += __shfl_xor(den, o);
   const float inv = 1.0f / den;
+  auto weight = [&](int i) { return i < n ? expf(range_lse(c0 + STEP * i) - mx) * inv : 0.0f; };
+  // lane i % 32 holds the weight of the half-wave's range i
   vec_t acc = 0.0f;
-  float wl = expf(l0 - mx) * inv;
+  float wl = weight(lane);
 #pragma unroll
-  for (int c = 0; c < kMergeAhead; ++c) {
-    const float wc = __shfl(wl, c, 32);
-    if (c < g.n_slots) acc += wc * ahead[c];
+  for (int i = 0; i < kMergeAhead; ++i) {
+    const float wc = __shfl(wl, i, 32);
+    if (i < n) acc += wc * ahead[i];
   }
-  for (int c = kMergeAhead; c < g.n_slots; ++c) {
-    if (c % 32 == 0) wl = expf(range_lse(c + lane) - mx) * inv;
-    acc += __shfl(wl, c % 32, 32) * part(c);
+  for (int i0 = kMergeAhead; i0 < n; i0 += kMergeAhead) {
+    if (i0 % 32 == 0) wl = weight(i0 + lane);
+#pragma unroll
+    for (int i = 0; i < kMergeAhead; ++i)
+      ahead[i] = part(i0 + i < n ? c0 + STEP * (i0 + i) : c0);
+#pragma unroll
+    for (int i = 0; i < kMergeAhead; ++i) {
+      const float wc = __shfl(wl, (i0 + i) % 32, 32);
+      if (i0 + i < n) acc += wc * ahead[i];
+    }
+  }
+  if constexpr (MANY) {
+    __shared__ vec_t sums[kMergeHalves][32];
+    sums[half][lane] = acc;
+    __syncthreads();
+    if (half > 0) return;
+#pragma unroll
+    for (int i = 1; i < kMergeHalves; ++i) acc += sums[i][lane];
   }
   const bool empty = row.pos < 0 || row.lo > row.pos;
   if (empty) acc = 0.0f;
@@ -651,7 +679,8 @@ hipError_t launch_step_attn(const tsr_step* p, const void* q, const void* req_k,
   const dim3 grid(p->n_items[0]), block(64 * kStepWaves);
   MergeArgs g{p->dev.rows, p->dev.merges, p->dev.split_o, p->dev.split_lse, out, lse,
               m.n_q_heads};
-  const dim3 mgrid(p->n_merges, kStepVecs / kMergeVecs);
+  const bool many = p->max_parts > kMergeAhead;
+  const dim3 mgrid(p->n_merges, many ? kStepVecs : kStepVecs / kMergeHalves);
 #define TSR_STEP(KERNEL, E, D)                                               \
   do {                                                                       \
     if (grid.x > 0) hipLaunchKernelGGL(KERNEL, grid, block, 0, s, a);        \
@@ -664,7 +693,12 @@ hipError_t launch_step_attn(const tsr_step* p, const void* q, const void* req_k,
       if (e != hipSuccess) return e;                                         \
     }                                                                        \
     if (p->n_merges == 0) return hipSuccess;                                 \
-    hipLaunchKernelGGL((step_merge_kernel<E, D>), mgrid, dim3(256), 0, s, g); \
+    if (many)                                                                \
+      hipLaunchKernelGGL((step_merge_kernel<E, D, true>), mgrid, dim3(32 * kMergeHalves), 0, s, \
+                         g);                                                 \
+    else                                                                     \
+      hipLaunchKernelGGL((step_merge_kernel<E, D, false>), mgrid, dim3(32 * kMergeHalves), 0, s, \
+                         g);                                                 \
     return hipGetLastError();                                                \
   } while (0)
   if (m.kv_dtype == TSR_BF16) TSR_STEP((step_attn_kernel<false>), uint16_t, kD);

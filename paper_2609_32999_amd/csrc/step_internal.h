@@ -45,10 +45,13 @@ struct alignas(16) StepItem {
   int32_t full_lo, full_hi;
   int32_t part_slot;  // -1: writes out and lse, else its first vector in the split buffer
   int32_t pad[2];
+  // pages of the 16-key blocks of tiles 0 .. 3, one tile for each wave: the
+  // first loads need not wait for the block table
+  int32_t pg[8];
 };
 
-// 16 vectors of an item whose key range was cut: vectors vec0 .. vec0 + 15 of
-// the item (rows row0 .., n_heads heads from hq0 on); range c's are at vector
+// 16 vectors of an item whose key range was cut (vectors vec0 .. vec0 + 15 of
+// the item: rows row0 .., n_heads heads from hq0 on); range c's are at vector
 // slot0 + c * stride of the split buffer.
 struct alignas(16) StepMerge {
   int32_t row0;
@@ -89,6 +92,7 @@ struct tsr_step {
   int32_t n_items[2];      // launch sizes: few rows, many rows (with padding)
   int32_t n_real_items;    // both, without
   int32_t n_split_items, n_merges;
+  int32_t max_parts;       // ranges of an item, at most
   bool shared_append;      // a row's page belongs to another request too
   size_t image_bytes, ws_bytes;
   size_t off_rows, off_items, off_merges, off_pages, off_bts, off_split_o, off_split_lse;

@@ -24,10 +24,25 @@ tsr_status fail_req(tsr_status st, int r, const std::string& msg) {
   return fail(st, "request " + std::to_string(r) + ": " + msg);
 }
 
-// A launch for few rows is cut into about this many items a compute unit, of
-// kMinRangeTiles tiles at least; one for many rows into one a unit.
-constexpr int kRangesPerCu = 3;
-constexpr int kMinRangeTiles = 8;
+// Key ranges of a launch for few rows.  A range costs its workgroup about 3 us
+// beside its tiles, and a merge the launch 2 us; alone on a unit a workgroup
+// needs 1.1 us for a round of four tiles, and a chip full of them 0.76 us a
+// tile of bf16 pages.  So, with 8 KV heads and one request:
+//   - items of up to kWholeRangeTiles tiles stay whole (8 tiles 6.3 us whole, 7.4
+//     in ranges of 2; 16 tiles 8.4 and 7.5);
+//   - else ranges as short as a range for each unit allows, 2 tiles at least (32
+//     tiles: 7.7 us in ranges of 2, 8.9 of 8, 12.7 whole; 128 tiles: 8.3 in 256
+//     ranges, 9.2 in 128, 11.3 in 512);
+//   - past kFewTiles tiles a range, as many as the units hold at once: one a
+//     unit for bf16 (1,032 tiles: 20 us in 256 ranges, 36 in 264, 35 in 520),
+//     three for 4-bit pages (18.7 us in 752, 21.1 in 264);
+//   - past kManyTiles, four times as many, where the lengths differ (16 prompts
+//     of 8,000 to 33,000 tokens, 64 heads: 218 us, 223 with two a unit).
+constexpr int kWholeRangeTiles = 12;
+constexpr int kMinRangeTiles = 2;
+constexpr int kFewTiles = 8;
+constexpr int kManyTiles = 40;
+// A launch for many rows: one range a unit, of 16 tiles at least.
 constexpr int kMinRowRangeTiles = 16;
 constexpr int64_t kMaxSplitVecs = (int64_t)1 << 21;
 // Requests with this many rows x heads go to the kernel for many rows.
@@ -88,6 +103,36 @@ StepItem cut(const StepItem& it, int32_t t0, int32_t t1) {
   c.b0 = it.b0 + std::max(t0 - na, 0);
   c.b1 = it.b0 + std::max(t1 - na, 0);
   return c;
+}
+
+// Smallest range length that leaves at most n_items items.
+int64_t tiles_for(const std::vector<StepItem>& whole, int64_t n_items) {
+  int64_t total = 0;
+  for (const StepItem& it : whole) total += n_tiles(it);
+  int64_t cap = std::max<int64_t>(1, (total + n_items - 1) / n_items);
+  while (cap < INT32_MAX) {
+    int64_t n = 0;
+    for (const StepItem& it : whole) n += std::max<int64_t>(1, (n_tiles(it) + cap - 1) / cap);
+    if (n <= n_items || n == (int64_t)whole.size()) break;
+    cap += 1 + cap / 16;
+  }
+  return cap;
+}
+
+int64_t range_tiles(const std::vector<StepItem>& whole, bool bf16) {
+  int64_t longest = 0;
+  for (const StepItem& it : whole) longest = std::max<int64_t>(longest, n_tiles(it));
+  if (longest <= kWholeRangeTiles) return INT32_MAX;
+  int64_t cap = std::max<int64_t>(kMinRangeTiles, tiles_for(whole, kNumCus));
+  if (cap <= kFewTiles) return cap;
+  const int64_t held = (bf16 ? 1 : 3) * kNumCus;
+  cap = std::max<int64_t>(kFewTiles, tiles_for(whole, held));
+  if (cap <= kManyTiles) return cap;
+  return std::max<int64_t>(kManyTiles, tiles_for(whole, 4 * kNumCus));
+}
+
+int64_t row_range_tiles(const std::vector<StepItem>& whole) {
+  return std::max<int64_t>(kMinRowRangeTiles, tiles_for(whole, kNumCus));
 }
 
 // Launch order: workgroups go to the XCDs in turn, so the list, in which
@@ -240,22 +285,25 @@ tsr_status build_step(const tsr_model* model, const tsr_step_request* reqs, int3
   if (whole[0].size() + whole[1].size() > (size_t)INT32_MAX / 64)
     return fail(TSR_ERR_OUT_OF_RANGE, "too many attention items");
 
+  // the page ids of an item's first tiles, one for each wave
+  auto first_pages = [&](StepItem* it) {
+    const int na = it->a1 - it->a0, nt = n_tiles(*it), last_blk = (it->kv_len - 1) & ~15;
+    for (int w = 0; w < 4 && w < nt; ++w)
+      for (int b = 0; b < 2; ++b) {
+        const int key = kStepKeys * (w < na ? it->a0 + w : it->b0 + w - na) + 16 * b;
+        it->pg[2 * w + b] = bts[it->bt_off + std::min(key, last_blk) / B];
+      }
+  };
   std::vector<StepItem> items;
   std::vector<StepMerge> merges;
   int64_t split_vecs = 0;
-  p->n_split_items = p->n_real_items = 0;
+  p->n_split_items = p->n_real_items = p->max_parts = 0;
   for (int kind = 0; kind < 2; ++kind) {
     const int most = kind ? kStepRowVecs : kStepVecs;
-    // key ranges
-    int64_t total = 0;
-    for (const StepItem& it : whole[kind]) total += n_tiles(it);
-    int64_t cap = INT32_MAX;
-    if (o.split_tiles > 0) cap = o.split_tiles;
-    if (o.split_tiles == 0) {
-      const int64_t want = (int64_t)(kind ? 1 : kRangesPerCu) * kNumCus;
-      cap = std::max<int64_t>(kind ? kMinRowRangeTiles : kMinRangeTiles,
-                              (total + want - 1) / want);
-    }
+    const int64_t cap = o.split_tiles > 0   ? o.split_tiles
+                        : o.split_tiles < 0 ? INT32_MAX
+                        : kind              ? row_range_tiles(whole[kind])
+                                            : range_tiles(whole[kind], m.kv_dtype == TSR_BF16);
     std::vector<StepItem> list;
     for (const StepItem& it : whole[kind]) {
       const int64_t n = n_tiles(it);
@@ -270,6 +318,7 @@ tsr_status build_step(const tsr_model* model, const tsr_step_request* reqs, int3
         continue;
       }
       ++p->n_split_items;
+      p->max_parts = std::max(p->max_parts, (int32_t)parts);
       for (int v = 0; v < it.n_rows * it.n_heads; v += kStepVecs)
         merges.push_back({it.row0, it.n_rows, it.kv_head * G + it.head0, it.n_heads,
                           (int32_t)split_vecs + v, (int32_t)parts, most, v});
@@ -281,6 +330,7 @@ tsr_status build_step(const tsr_model* model, const tsr_step_request* reqs, int3
       split_vecs += parts * most;
     }
     p->n_real_items += (int32_t)list.size();
+    for (StepItem& it : list) first_pages(&it);
     const size_t before = items.size();
     schedule(list, &items);
     p->n_items[kind] = (int32_t)(items.size() - before);
