@@ -20,13 +20,13 @@ struct AppendArgs {
   uint8_t* req_scale;
   const float *rope_cos, *rope_sin;
   int64_t q_stride, k_stride, v_stride;
-  int32_t T, n_q_heads, n_kv_heads, log2_page, units;
+  int32_t T, n_q_heads, n_kv_heads, log2_page;
   float eps;
   bool norm;
 };
 
-// One block of 32 dims of a head, 8 of them in each of four lanes, as codes
-// and a scale byte.  `at`: the head's element offset / 32 in the pages.
+// One block of 32 dims of a token's head, 8 of them in each of four lanes, as
+// codes and a scale byte; `head`: which (page, KV head, slot) of the pages.
 __device__ __forceinline__ void put_e2m1(const float* x, int c, int block, int64_t head,
                                          uint8_t* codes, uint8_t* scale) {
   float amax = 0.0f;
@@ -48,120 +48,108 @@ __device__ __forceinline__ void put_e2m1(const float* x, int c, int block, int64
   if ((c & 3) == 0) scale[block] = (uint8_t)b;
 }
 
-// A group of D / 16 lanes takes one head vector: lane c holds dims 8 c .. and
-// D/2 + 8 c .., the two members of eight RoPE pairs, so that the norm is
-// one sum over the group and the rotation stays in the lane.  The group's N
-// vectors are of one row (heads j, j + units, ...: query heads, then key and
-// value heads), so its cos and sin are read once.
-template <typename E, int KIND, int D, int N>
+// Eight values to memory, bf16 in the hardware's rounding (to nearest even).
+__device__ __forceinline__ void put8(float* p, const float* x) { store8(p, x); }
+__device__ __forceinline__ void put8(uint16_t* p, const float* x) {
+  *reinterpret_cast<uint4*>(p) = make_uint4(pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]),
+                                            pack_bf16x2(x[4], x[5]), pack_bf16x2(x[6], x[7]));
+}
+
+// A group of D / 16 lanes takes one head vector of one row: lane c holds dims
+// 8 c .. and D/2 + 8 c .., the two members of eight RoPE pairs, so that the
+// norm is one sum over the group and the rotation stays in the lane.
+//
+// Bound by HBM.  A vector a group, and as many groups as there are vectors:
+// several vectors a group, to read the row's cos and sin once, left fewer
+// loads in flight (14,892 rows, 32 + 16 heads of 128: 77 us, 5.3 TB/s, with
+// one; 80, 84, 88 and 92 with 2, 3, 4 and 6).
+template <typename E, int KIND, int D>
 __global__ __launch_bounds__(256) void step_append_kernel(const AppendArgs a) {
   constexpr int L = D / 16, H = D / 2;
+  const int nq = a.n_q_heads, nk = a.n_kv_heads, n_vec = nq + 2 * nk;
   const int c = threadIdx.x % L;
   const int64_t grp = (int64_t)blockIdx.x * (256 / L) + threadIdx.x / L;
-  const int64_t t64 = grp / a.units;
-  if (t64 >= a.T) return;   // whole groups leave together
-  const int t = (int)t64, j = (int)(grp % a.units);
-  const int nq = a.n_q_heads, nk = a.n_kv_heads, n_vec = nq + 2 * nk;
+  if (grp >= (int64_t)a.T * n_vec) return;   // whole groups leave together
+  const int t = (int)(grp / n_vec), h = (int)(grp - (int64_t)t * n_vec);
   const StepRow row = a.rows[t];
   if (row.pos < 0) return;
+  const bool is_q = h < nq, is_v = h >= nq + nk;
+  const int g = h - nq - (is_v ? nk : 0);       // KV head
 
-  float x[N][16];
+  const E* src = is_q   ? static_cast<const E*>(a.q) + t * a.q_stride + (int64_t)h * D
+                 : is_v ? static_cast<const E*>(a.v) + t * a.v_stride + (int64_t)g * D
+                        : static_cast<const E*>(a.k) + t * a.k_stride + (int64_t)g * D;
+  float x[16];
+  load8(src + 8 * c, x);
+  load8(src + H + 8 * c, x + 8);
+  if (!is_v) {
+    float cs[8], sn[8];
+    load8(a.rope_cos + (int64_t)row.pos * H + 8 * c, cs);
+    load8(a.rope_sin + (int64_t)row.pos * H + 8 * c, sn);
+    if (a.norm) {
+      const E* w = static_cast<const E*>(is_q ? a.q_weight : a.k_weight);
+      float wv[16];
 #pragma unroll
-  for (int i = 0; i < N; ++i) {
-    const int h = j + i * a.units;
-    if (h >= n_vec) break;
-    const E* src = h < nq        ? static_cast<const E*>(a.q) + t * a.q_stride + (int64_t)h * D
-                   : h < nq + nk ? static_cast<const E*>(a.k) + t * a.k_stride + (int64_t)(h - nq) * D
-                                 : static_cast<const E*>(a.v) + t * a.v_stride +
-                                       (int64_t)(h - nq - nk) * D;
-    load8(src + 8 * c, x[i]);
-    load8(src + H + 8 * c, x[i] + 8);
+      for (int e = 0; e < 16; ++e) wv[e] = 1.0f;
+      if (w) {
+        load8(w + 8 * c, wv);
+        load8(w + H + 8 * c, wv + 8);
+      }
+      float s = 0.0f;
+#pragma unroll
+      for (int e = 0; e < 16; ++e) s = fmaf(x[e], x[e], s);
+#pragma unroll
+      for (int o = 1; o < L; o <<= 1) s += __shfl_xor(s, o);
+      const float r = 1.0f / sqrtf(s * (1.0f / D) + a.eps);
+#pragma unroll
+      for (int e = 0; e < 16; ++e) x[e] = x[e] * r * wv[e];
+    }
+    if (!is_q) {
+      // the form a unit cache keeps; K is rotated from it, so that a unit
+      // composed from the cache holds the same bits
+      if constexpr (sizeof(E) == 2) {
+#pragma unroll
+        for (int e = 0; e < 16; e += 2) {
+          const uint32_t u = pack_bf16x2(x[e], x[e + 1]);
+          x[e] = __uint_as_float(u << 16);
+          x[e + 1] = __uint_as_float(u & 0xffff0000u);
+        }
+      }
+      if (a.k_pre) {
+        E* dst = static_cast<E*>(a.k_pre) + ((int64_t)t * nk + g) * D;
+        put8(dst + 8 * c, x);
+        put8(dst + H + 8 * c, x + 8);
+      }
+    }
+    rope_rotate<8>(x, x + 8, cs, sn);
   }
-  float cs[8], sn[8];
-  load8(a.rope_cos + (int64_t)row.pos * H + 8 * c, cs);
-  load8(a.rope_sin + (int64_t)row.pos * H + 8 * c, sn);
-
-#pragma unroll
-  for (int i = 0; i < N; ++i) {
-    const int h = j + i * a.units;
-    if (h >= n_vec) break;
-    const bool is_q = h < nq, is_v = h >= nq + nk;
-    const int g = h - nq - (is_v ? nk : 0);       // KV head
-    if (!is_v) {
-      if (a.norm) {
-        float s = 0.0f;
-#pragma unroll
-        for (int e = 0; e < 16; ++e) s = fmaf(x[i][e], x[i][e], s);
-#pragma unroll
-        for (int o = 1; o < L; o <<= 1) s += __shfl_xor(s, o);
-        const float r = 1.0f / sqrtf(s * (1.0f / D) + a.eps);
-        const E* w = static_cast<const E*>(is_q ? a.q_weight : a.k_weight);
-        if (w) {
-          float wv[16];
-          load8(w + 8 * c, wv);
-          load8(w + H + 8 * c, wv + 8);
-#pragma unroll
-          for (int e = 0; e < 16; ++e) x[i][e] = x[i][e] * r * wv[e];
-        } else {
-#pragma unroll
-          for (int e = 0; e < 16; ++e) x[i][e] *= r;
-        }
-      }
-      if (!is_q) {
-        // the form a unit cache keeps; K is rotated from it, so that a unit
-        // composed from the cache holds the same bits
-        if constexpr (sizeof(E) == 2) {
-#pragma unroll
-          for (int e = 0; e < 16; ++e) x[i][e] = bf16_to_f32(f32_to_bf16(x[i][e]));
-        }
-        if (a.k_pre) {
-          E* dst = static_cast<E*>(a.k_pre) + ((int64_t)t * nk + g) * D;
-          store8(dst + 8 * c, x[i]);
-          store8(dst + H + 8 * c, x[i] + 8);
-        }
-      }
-      rope_rotate<8>(x[i], x[i] + 8, cs, sn);
-    }
-    if (is_q) {
-      E* dst = static_cast<E*>(a.q_out) + ((int64_t)t * nq + h) * D;
-      store8(dst + 8 * c, x[i]);
-      store8(dst + H + 8 * c, x[i] + 8);
-      continue;
-    }
-    const int64_t head = ((((int64_t)(row.dst >> a.log2_page) * nk + g) << a.log2_page) +
-                          (row.dst & ((1 << a.log2_page) - 1)));
-    void* pages = is_v ? a.req_v : a.req_k;
-    if constexpr (KIND == kPageE2m1) {
-      const int64_t page = row.dst >> a.log2_page;
-      const int64_t sc = ((((page * 2 + is_v) * nk + g) << a.log2_page) +
-                          (row.dst & ((1 << a.log2_page) - 1)));
-      uint8_t* scale = a.req_scale + sc * (D / kScaleDims);
-      put_e2m1(x[i], c, c / 4, head, static_cast<uint8_t*>(pages), scale);
-      put_e2m1(x[i] + 8, c, D / 64 + c / 4, head, static_cast<uint8_t*>(pages), scale);
-    } else {
-      E* dst = static_cast<E*>(pages) + head * D;
-      store8(dst + 8 * c, x[i]);
-      store8(dst + H + 8 * c, x[i] + 8);
-    }
+  if (is_q) {
+    E* dst = static_cast<E*>(a.q_out) + ((int64_t)t * nq + h) * D;
+    put8(dst + 8 * c, x);
+    put8(dst + H + 8 * c, x + 8);
+    return;
+  }
+  const int64_t page = row.dst >> a.log2_page, slot = row.dst & ((1 << a.log2_page) - 1);
+  const int64_t head = ((page * nk + g) << a.log2_page) + slot;
+  void* pages = is_v ? a.req_v : a.req_k;
+  if constexpr (KIND == kPageE2m1) {
+    uint8_t* scale = a.req_scale + ((((page * 2 + is_v) * nk + g) << a.log2_page) + slot) *
+                                       (D / kScaleDims);
+    put_e2m1(x, c, c / 4, head, static_cast<uint8_t*>(pages), scale);
+    put_e2m1(x + 8, c, D / 64 + c / 4, head, static_cast<uint8_t*>(pages), scale);
+  } else {
+    E* dst = static_cast<E*>(pages) + head * D;
+    put8(dst + 8 * c, x);
+    put8(dst + H + 8 * c, x + 8);
   }
 }
 
 template <typename E, int KIND, int D>
-hipError_t run_append(AppendArgs a, hipStream_t s) {
-  const int n_vec = a.n_q_heads + 2 * a.n_kv_heads;
-  auto blocks = [&](int units) {
-    return (unsigned)(((int64_t)a.T * units + 256 / (D / 16) - 1) / (256 / (D / 16)));
-  };
-  constexpr int N = 4;
-  a.units = (n_vec + N - 1) / N;
-  if (blocks(a.units) >= 4 * kNumCus) {
-    hipLaunchKernelGGL((step_append_kernel<E, KIND, D, N>), dim3(blocks(a.units)), dim3(256), 0, s,
-                       a);
-  } else {
-    a.units = n_vec;
-    hipLaunchKernelGGL((step_append_kernel<E, KIND, D, 1>), dim3(blocks(a.units)), dim3(256), 0, s,
-                       a);
-  }
+hipError_t run_append(const AppendArgs& a, hipStream_t s) {
+  const int64_t groups = (int64_t)a.T * (a.n_q_heads + 2 * a.n_kv_heads);
+  constexpr int kGroups = 256 / (D / 16);
+  hipLaunchKernelGGL((step_append_kernel<E, KIND, D>), dim3((groups + kGroups - 1) / kGroups),
+                     dim3(256), 0, s, a);
   return hipGetLastError();
 }
 

@@ -373,7 +373,7 @@ def test_append(kv, hq, hkv, d, page, weights, norm):
 
 
 def test_append_many_rows_equal_few():
-    """The launch for many rows gives the bits of the one for few."""
+    """Rows appended all at once and 50 at a time: the same bits."""
     sh = shape(32, 8, max_position=65536)
     g = gen(4)
     T = 700
