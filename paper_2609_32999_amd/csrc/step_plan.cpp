@@ -42,11 +42,26 @@ constexpr int kWholeRangeTiles = 12;
 constexpr int kMinRangeTiles = 2;
 constexpr int kFewTiles = 8;
 constexpr int kManyTiles = 40;
-// A launch for many rows: one range a unit, of 16 tiles at least.
-constexpr int kMinRowRangeTiles = 16;
 constexpr int64_t kMaxSplitVecs = (int64_t)1 << 21;
-// Requests with this many rows x heads go to the kernel for many rows.
-constexpr int kManyVecs = 64;
+
+// What a launch lasts, in us, for the choice between the two kernels and of
+// the second one's ranges.  Few rows: kFewUs and a tile's time on each unit
+// (bf16 pages 0.35 us, 4-bit 0.19).  Many rows: kManyUs, a tile's on each unit,
+// and for every range what its 256 partial rows cost to write and to merge; or
+// the longest range alone.  Measured and so estimated, 32 query heads, 4,096
+// keys: 16 requests of 8 rows 64 and 50 with the first, 74 and 82 with the
+// second; of 16 rows 100 and 95, 78 and 85; of 64 rows 314 and 365, 106 and 105;
+// one request of 64 rows 30 and 27, 35 and 28; of 128 rows 54 and 50, 39 and 36;
+// over 4-bit pages 16 requests of 16 rows 58 and 54, 72 and 85; of 32 rows 97 and
+// 102, 80 and 92.
+constexpr double kFewUs = 5, kFewTileUs = 0.35, kFewTileUs4 = 0.19;
+constexpr double kManyUs = 15, kManyTileUs = 1.0, kManyLoneTileUs = 1.17, kManyStartUs = 4;
+constexpr double kManyPartUs = 13;
+// Range lengths tried for the second kernel, in tiles.
+constexpr int kManyCaps[] = {8, 12, 16, 24, 32, 48, 64, 96, 128, 256};
+// Requests with this many rows x heads always go to the second kernel; up to an
+// item of the first kernel, to that.
+constexpr int64_t kAlwaysManyVecs = 2048;
 
 // Key tiles [a0, a1) and [b0, b1) that hold every key some row of
 // rows[r0 .. r0 + n) sees, and the keys visible to all of them.
@@ -131,8 +146,32 @@ int64_t range_tiles(const std::vector<StepItem>& whole, bool bf16) {
   return std::max<int64_t>(kManyTiles, tiles_for(whole, 4 * kNumCus));
 }
 
-int64_t row_range_tiles(const std::vector<StepItem>& whole) {
-  return std::max<int64_t>(kMinRowRangeTiles, tiles_for(whole, kNumCus));
+// The second kernel's launch time with ranges of at most `cap` tiles.
+double many_us(const std::vector<StepItem>& whole, int64_t cap) {
+  double work = 0;
+  int64_t longest = 0;
+  for (const StepItem& it : whole) {
+    const int64_t n = n_tiles(it), parts = std::max<int64_t>(1, (n + cap - 1) / cap);
+    work += kManyTileUs * n;
+    if (parts > 1) work += kManyPartUs * parts * it.n_rows * it.n_heads / kStepRowVecs;
+    longest = std::max(longest, (n + parts - 1) / parts);
+  }
+  return kManyUs + std::max(work / kNumCus, kManyLoneTileUs * longest + kManyStartUs);
+}
+
+// The range length it is shortest with, INT32_MAX for whole items.
+int64_t row_range_tiles(const std::vector<StepItem>& whole, double* us) {
+  int64_t best = INT32_MAX;
+  *us = whole.empty() ? 0 : many_us(whole, best);
+  for (int cap : kManyCaps)
+    if (!whole.empty()) {
+      const double t = many_us(whole, cap);
+      if (t < *us) {
+        *us = t;
+        best = cap;
+      }
+    }
+  return best;
 }
 
 // Launch order: workgroups go to the XCDs in turn, so the list, in which
@@ -258,29 +297,83 @@ tsr_status build_step(const tsr_model* model, const tsr_step_request* reqs, int3
     if (page_n[i]) pages.push_back({i, page_n[i]});
 
   // attention items: row tile x head block x KV head, of either kernel
-  std::vector<StepItem> whole[2];
-  for (int r = 0; r < n_req; ++r) {
-    const int64_t vecs = (int64_t)(row0[r + 1] - row0[r]) * G;
-    const int kind = o.attn_kernel ? o.attn_kernel - 1
-                                   : m.act_dtype == TSR_BF16 && vecs >= kManyVecs;
+  auto add_items = [&](int r, int kind, std::vector<StepItem>* out) {
     const int most = kind ? kStepRowVecs : kStepVecs;
     const int hb = std::min(G, most);              // heads of an item
     const int rt = most / hb;                      // rows of an item
+    const size_t first = out->size();
+    for (int i = row0[r]; i < row0[r + 1]; i += rt) {
+      StepItem it{};
+      it.row0 = i;
+      it.n_rows = std::min(rt, row0[r + 1] - i);
+      it.bt_off = bt_off[r];
+      it.kv_len = reqs[r].kv_len;
+      it.part_slot = -1;
+      item_keys(rows, i, it.n_rows, o, &it);
+      out->push_back(it);
+    }
+    const std::vector<StepItem> tiles(out->begin() + first, out->end());
+    out->resize(first);
     for (int g = 0; g < Hkv; ++g)
       for (int h = 0; h < G; h += hb)
-        for (int i = row0[r]; i < row0[r + 1]; i += rt) {
-          StepItem it{};
-          it.row0 = i;
-          it.n_rows = std::min(rt, row0[r + 1] - i);
-          it.bt_off = bt_off[r];
-          it.kv_len = reqs[r].kv_len;
-          it.part_slot = -1;
+        for (StepItem it : tiles) {
           it.kv_head = g;
           it.head0 = h;
           it.n_heads = std::min(hb, G - h);
-          item_keys(rows, i, it.n_rows, o, &it);
-          whole[kind].push_back(it);
+          out->push_back(it);
         }
+  };
+  std::vector<StepItem> whole[2];
+  std::vector<int> either;   // requests that both kernels may serve
+  for (int r = 0; r < n_req; ++r) {
+    const int64_t vecs = (int64_t)(row0[r + 1] - row0[r]) * G;
+    if (o.attn_kernel || m.act_dtype != TSR_BF16 || vecs <= kStepVecs ||
+        vecs >= kAlwaysManyVecs) {
+      const int kind = o.attn_kernel ? o.attn_kernel - 1
+                                     : m.act_dtype == TSR_BF16 && vecs >= kAlwaysManyVecs;
+      add_items(r, kind, &whole[kind]);
+    } else {
+      either.push_back(r);
+    }
+  }
+  if (!either.empty()) {
+    // those with most rows go to the second kernel, down to the count with
+    // which the two launches are shortest
+    std::stable_sort(either.begin(), either.end(), [&](int a, int b) {
+      return row0[a + 1] - row0[a] > row0[b + 1] - row0[b];
+    });
+    const double tile_us = m.kv_dtype == TSR_BF16 ? kFewTileUs : kFewTileUs4;
+    std::vector<std::vector<StepItem>> few(either.size());
+    double work = 0;
+    for (const StepItem& it : whole[0]) work += n_tiles(it);
+    for (size_t i = 0; i < either.size(); ++i) {
+      add_items(either[i], 0, &few[i]);
+      for (const StepItem& it : few[i]) work += n_tiles(it);
+    }
+    std::vector<StepItem> many = whole[1];
+    double best = 0;
+    size_t best_n = 0;
+    for (size_t n = 0;; ++n) {   // the first n to the second kernel
+      // (counts that are not a power of two of them, or all, are not tried)
+      if (n == either.size() || (n & (n - 1)) == 0) {
+        double us;
+        row_range_tiles(many, &us);
+        if (work > 0 || !whole[0].empty() || n < either.size())
+          us += kFewUs + tile_us * work / kNumCus;
+        if (n == 0 || us < best) {
+          best = us;
+          best_n = n;
+        }
+      }
+      if (n == either.size()) break;
+      for (const StepItem& it : few[n]) work -= n_tiles(it);
+      add_items(either[n], 1, &many);
+    }
+    for (size_t i = 0; i < either.size(); ++i)
+      if (i < best_n)
+        add_items(either[i], 1, &whole[1]);
+      else
+        whole[0].insert(whole[0].end(), few[i].begin(), few[i].end());
   }
   if (whole[0].size() + whole[1].size() > (size_t)INT32_MAX / 64)
     return fail(TSR_ERR_OUT_OF_RANGE, "too many attention items");
@@ -300,9 +393,10 @@ tsr_status build_step(const tsr_model* model, const tsr_step_request* reqs, int3
   p->n_split_items = p->n_real_items = p->max_parts = 0;
   for (int kind = 0; kind < 2; ++kind) {
     const int most = kind ? kStepRowVecs : kStepVecs;
+    double us;
     const int64_t cap = o.split_tiles > 0   ? o.split_tiles
                         : o.split_tiles < 0 ? INT32_MAX
-                        : kind              ? row_range_tiles(whole[kind])
+                        : kind              ? row_range_tiles(whole[kind], &us)
                                             : range_tiles(whole[kind], m.kv_dtype == TSR_BF16);
     std::vector<StepItem> list;
     for (const StepItem& it : whole[kind]) {

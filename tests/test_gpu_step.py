@@ -177,7 +177,7 @@ CASES = {
     "many_window_one": (dict(), [(140, 140)], dict(window=1, n_sinks=1)),
     "many_cut": (dict(), [(900, 90)], dict(split_tiles=3)),
     "many_cut_window": (dict(), [(900, 300)], dict(split_tiles=2, window=100, n_sinks=40)),
-    "many_and_few": (dict(), [(900, 1), (333, 200), (77, 2), (90, 16)], dict()),
+    "many_and_few": (dict(), [(900, 1), (700, 600), (77, 2), (90, 16)], dict()),
     "many_mha": (dict(hq=2, hkv=2), [(530, 530)], dict(window=300)),
     "many_g5": (dict(hq=10, hkv=2), [(260, 130), (64, 20)], dict()),
     "many_g20": (dict(hq=20, hkv=1), [(99, 50)], dict()),
@@ -202,7 +202,7 @@ CASES = {
 
 
 @pytest.mark.parametrize("name,kernel", [(n, 0) for n in CASES] +
-                         [(n, 2) for n in CASES if n[:3] != "f32" and n[:4] != "many"] +
+                         [(n, 2) for n in CASES if n[:3] != "f32"] +
                          [(n, 1) for n in CASES if n[:4] == "many"])
 def test_attention(name, kernel):
     sh, lens, opt = CASES[name]
@@ -513,7 +513,7 @@ FOUR_BIT = ["many", "many_window", "many_cut_window", "many_and_few", "many_g5",
 
 
 @pytest.mark.parametrize("name,kernel", [(n, 0) for n in FOUR_BIT] +
-                         [(n, 2) for n in FOUR_BIT if n[:4] != "many"])
+                         [(n, 2) for n in FOUR_BIT])
 def test_four_bit_attention(name, kernel):
     sh, lens, opt = CASES[name]
     sh, opt = shape(**sh), dict(opt, attn_kernel=kernel)

@@ -154,15 +154,31 @@ def test_few_row_items():
 def test_many_row_items():
     # 256 rows x heads an item: 64 rows of 4 heads
     m = model(hq=8, hkv=2)
-    s = make([req(kv_len=200, n_rows=130)], split_tiles=-1)
+    s = make([req(kv_len=200, n_rows=130)], split_tiles=-1, attn_kernel=2)
     assert s.attn_item_rows == 256 and s.num_attn_items == 2 * 3
-    # a request with few rows beside it keeps the other kernel's items
-    s = make([req(kv_len=200, n_rows=130), req(kv_len=40, n_rows=1, first=20)], split_tiles=-1)
-    assert s.attn_item_rows == 256 and s.num_attn_items == 2 * 3 + 2
-    assert make([req(kv_len=200, n_rows=2)], m).attn_item_rows == 16
     assert make([req(kv_len=200, n_rows=2)], m, attn_kernel=2).attn_item_rows == 256
     refused(P.TSR_ERR_UNSUPPORTED, "bf16 activations only", m=model(kv="f32"), attn_kernel=2)
     assert make([req(kv_len=200, n_rows=130)], model(kv="f32")).attn_item_rows == 16
+
+
+@pytest.mark.parametrize("kv", ["bf16", "e2m1"])
+def test_kernel_by_rows(kv):
+    """Few rows go to the one, many to the other, each request by itself."""
+    m = model(32, 8, kv=kv)
+    n = 4096 // 16
+
+    def auto(rows):
+        return make([req(kv_len=4096, n_rows=r, first=i * n) for i, r in enumerate(rows)], m,
+                    n * len(rows))
+
+    assert auto([1] * 4).attn_item_rows == 16
+    assert auto([2000]).attn_item_rows == 256
+    # 16 requests of 64 rows: 256 row x head vectors each, a launch that fills the chip
+    assert auto([64] * 16).attn_item_rows == 256
+    # a long extension beside decoding requests: both kinds of item
+    both, long, few = auto([2000, 1, 1]), auto([2000]), auto([1, 1])
+    assert both.attn_item_rows == 256
+    assert both.num_attn_items == long.num_attn_items + few.num_attn_items
 
 
 def test_key_ranges():
