@@ -209,11 +209,11 @@ __global__ __launch_bounds__(64 * kStepWaves, F4 ? 3 : 1) void step_attn_kernel(
     }
     const bool masked = key0 < it.full_lo || key0 + kStepKeys - 1 > it.full_hi;
     if (masked) {
+      const uint32_t bits = seen_bits(sight, key0) >> (4 * c4);
 #pragma unroll
       for (int b = 0; b < 2; ++b)
 #pragma unroll
-        for (int r = 0; r < 4; ++r)
-          if (!sees(sight, key0 + 16 * b + 4 * c4 + r)) s[b][r] = -INFINITY;
+        for (int r = 0; r < 4; ++r) s[b][r] = where_bit(bits, 16 * b + r, s[b][r]);
     }
     // ---- online softmax.  The running maximum m (common to the four lanes of
     // a vector) moves only when the probabilities taken against it grow past

@@ -40,6 +40,21 @@ __device__ __forceinline__ bool sees(const Sight& s, int key) {
   return (key <= s.pos) & (key >= s.lo) & ((key >= s.wlo) | (key < s.shi));
 }
 
+// Bit i: whether key0 + i is seen, i < 32.  (Per score, four comparisons and
+// their combination took more than the two products of a tile.)
+__device__ __forceinline__ uint32_t seen_bits(const Sight& s, int key0) {
+  auto from = [&](int key) {   // keys >= key
+    const int d = min(max(key - key0, 0), 32);
+    return (uint32_t)(0xffffffffull << d);
+  };
+  return from(s.lo) & ~from(s.pos + 1) & (from(s.wlo) | ~from(s.shi));
+}
+// x where bit `i` of bits is set, else -infinity.
+__device__ __forceinline__ float where_bit(uint32_t bits, int i, float x) {
+  const uint32_t all = (uint32_t)((int32_t)(bits << (31 - i)) >> 31);
+  return __uint_as_float((__float_as_uint(x) & all) | (0xff800000u & ~all));
+}
+
 // A uniform 32-bit load through the scalar cache.
 __device__ __forceinline__ int32_t uniform_i32(const int32_t* p) {
   return *reinterpret_cast<const __attribute__((address_space(4))) int32_t*>(

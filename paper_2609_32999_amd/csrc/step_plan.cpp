@@ -46,17 +46,22 @@ constexpr int64_t kMaxSplitVecs = (int64_t)1 << 21;
 
 // What a launch lasts, in us, for the choice between the two kernels and of
 // the second one's ranges.  Few rows: kFewUs and a tile's time on each unit
-// (bf16 pages 0.35 us, 4-bit 0.19).  Many rows: kManyUs, a tile's on each unit,
-// and for every range what its 256 partial rows cost to write and to merge; or
-// the longest range alone.  Measured and so estimated, 32 query heads, 4,096
-// keys: 16 requests of 8 rows 64 and 50 with the first, 74 and 82 with the
-// second; of 16 rows 100 and 95, 78 and 85; of 64 rows 314 and 365, 106 and 105;
-// one request of 64 rows 30 and 27, 35 and 28; of 128 rows 54 and 50, 39 and 36;
-// over 4-bit pages 16 requests of 16 rows 58 and 54, 72 and 85; of 32 rows 97 and
-// 102, 80 and 92.
+// (bf16 pages 0.35 us, 4-bit 0.19).  Many rows: kManyUs, for every range what
+// its 256 partial rows cost each unit to write and to merge, and the longer of
+// the longest range alone and a unit's share of them.  Measured and so
+// estimated, 32 query heads, 4,096 keys:
+//                           first kernel    second
+//   16 requests of 8 rows     64    50     74    79
+//                 of 16       99    95     82    82
+//                 of 64      314   364    109   104
+//   1 request of 64 rows      30    27     33    27
+//                of 128       54    50     36    34
+//                of 256       88    95     41    44
+//   4-bit, 16 of 16 rows      57    54     85    82
+//              of 32          97   102     80    90
 constexpr double kFewUs = 5, kFewTileUs = 0.35, kFewTileUs4 = 0.19;
-constexpr double kManyUs = 15, kManyTileUs = 1.0, kManyLoneTileUs = 1.17, kManyStartUs = 4;
-constexpr double kManyPartUs = 13;
+constexpr double kManyUs = 10, kManyTileUs = 1.0, kManyLoneTileUs = 1.17;
+constexpr double kManyPartUs = 15;
 // Range lengths tried for the second kernel, in tiles.
 constexpr int kManyCaps[] = {8, 12, 16, 24, 32, 48, 64, 96, 128, 256};
 // Requests with this many rows x heads always go to the second kernel; up to an
@@ -148,15 +153,18 @@ int64_t range_tiles(const std::vector<StepItem>& whole, bool bf16) {
 
 // The second kernel's launch time with ranges of at most `cap` tiles.
 double many_us(const std::vector<StepItem>& whole, int64_t cap) {
-  double work = 0;
-  int64_t longest = 0;
+  double tiles = 0, partial = 0;
+  int64_t longest = 0, items = 0;
   for (const StepItem& it : whole) {
     const int64_t n = n_tiles(it), parts = std::max<int64_t>(1, (n + cap - 1) / cap);
-    work += kManyTileUs * n;
-    if (parts > 1) work += kManyPartUs * parts * it.n_rows * it.n_heads / kStepRowVecs;
+    tiles += n;
+    items += parts;
+    if (parts > 1) partial += (double)parts * it.n_rows * it.n_heads / kStepRowVecs;
     longest = std::max(longest, (n + parts - 1) / parts);
   }
-  return kManyUs + std::max(work / kNumCus, kManyLoneTileUs * longest + kManyStartUs);
+  const int64_t rounds = (items + kNumCus - 1) / kNumCus;   // items of a unit
+  const double share = rounds > 1 ? kManyTileUs * rounds * tiles / items : 0;
+  return kManyUs + kManyPartUs * partial / kNumCus + std::max(kManyLoneTileUs * longest, share);
 }
 
 // The range length it is shortest with, INT32_MAX for whole items.

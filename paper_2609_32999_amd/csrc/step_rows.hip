@@ -282,10 +282,9 @@ __global__ __launch_bounds__(64 * kRowWaves, 2) void step_rows_kernel(const Step
     };
     auto softmax = [&](int b) __attribute__((always_inline)) {
       if constexpr (MASK) {
-        const Sight sight = sights[64 * w + 32 * b + l32];
+        const uint32_t bits = seen_bits(sights[64 * w + 32 * b + l32], key0) >> (4 * lh);
 #pragma unroll
-        for (int r = 0; r < 16; ++r)
-          s[b][r] = sees(sight, key0 + 8 * (r >> 2) + 4 * lh + (r & 3)) ? s[b][r] : -INFINITY;
+        for (int r = 0; r < 16; ++r) s[b][r] = where_bit(bits, 8 * (r >> 2) + (r & 3), s[b][r]);
       }
       probabilities(b);
     };
