@@ -35,8 +35,8 @@
  * (UNSUPPORTED): their one scale a page would have to change, and the page
  * with it, for every token appended.
  *
- * Pointers to K, V, q, out, codes and scales must be 16-byte aligned, lse and
- * k_pre likewise.  The current device must be the one the buffers are on.
+ * Pointers to activations, pages and scales must be 16-byte aligned.  The
+ * current device must be the one the buffers are on.
  */
 #ifndef TSR_STEP_H
 #define TSR_STEP_H
@@ -163,7 +163,7 @@ tsr_status tsr_step_append(const tsr_step* step, const tsr_qk_norm* norm, const 
 /* o_t,h = softmax(scale * q_t,h . K_j,g) V_j,g over the visible keys j, g =
  * h / (n_q_heads / n_kv_heads), lse its natural log-sum-exp.
  *   q     device [T][n_q_heads][head_dim], rotated (tsr_step_append's q_out).
- *   out   device [T][n_q_heads][head_dim] of act dtype.
+ *   out   device [T][n_q_heads][head_dim] of act dtype; may be q.
  *   lse   device [T][n_q_heads] fp32, or NULL.
  * Every position that a row sees must have been written.  Keys that a row
  * does not see do not reach its output, whatever they hold.  Scores and sums
@@ -172,8 +172,10 @@ tsr_status tsr_step_append(const tsr_step* step, const tsr_qk_norm* norm, const 
  * bound by reading the pages) the probabilities enter the second product as
  * two bf16 parts.  For many (256 an item, bound by the matrix cores) they and
  * the values enter it as fp16: a value beyond 65504 in magnitude makes the
- * outputs that see it non-finite.  The second serves steps whose requests
- * have rows enough to fill its items. */
+ * outputs that see it non-finite.  With attn_kernel 0 each request goes to
+ * the one its rows are sooner done with.  Results do not depend on the order
+ * in which the launch runs; they differ in rounding between the kernels and
+ * between key ranges. */
 tsr_status tsr_step_attn(const tsr_step* step, const void* q, const void* req_k,
                          const void* req_v, const void* req_scale, void* out, float* lse,
                          void* stream);

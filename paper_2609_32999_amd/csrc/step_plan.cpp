@@ -293,7 +293,7 @@ tsr_status build_step(const tsr_model* model, const tsr_step_request* reqs, int3
       }
       rows.push_back(row);
     }
-    if (rows.size() > (size_t)INT32_MAX / 64 / 256)
+    if (rows.size() > (size_t)1 << 24)
       return fail(TSR_ERR_OUT_OF_RANGE, "too many rows");
     row0[r + 1] = (int32_t)rows.size();
   }
@@ -641,7 +641,9 @@ tsr_status tsr_step_attn(const tsr_step* p, const void* q, const void* req_k,
     if ((st = check_scale(p, req_scale)) != TSR_OK) return st;
     if (p->T == 0) return TSR_OK;
     if (!q || !req_k || !req_v || !out) return null_pointer("step_attn");
-    if (!aligned({q, req_k, req_v, req_scale, out, lse})) return misaligned();
+    if (!aligned({q, req_k, req_v, req_scale, out})) return misaligned();
+    if (reinterpret_cast<uintptr_t>(lse) % 4)
+      return fail(TSR_ERR_INVALID_ARG, "lse is not 4-byte aligned");
     hipError_t e = launch_step_attn(p, q, req_k, req_v, req_scale, out, lse,
                                     static_cast<hipStream_t>(stream));
     if (e != hipSuccess) return device_fail("step attention launch", e);

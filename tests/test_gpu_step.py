@@ -627,6 +627,26 @@ def test_composed_rows_equal_the_plan_attention():
     assert ((out - out2).float().norm() / out2.float().norm()) < 4e-3
 
 
+@pytest.mark.parametrize("kernel", [1, 2])
+def test_out_in_place_and_shared_prefix(kernel):
+    """out may be q; requests may share the pages of a common prefix, also
+    when the pages after it are appended to."""
+    sh = shape(8, 2)
+    reqs, n = batch([(70, 3), (50, 2)], 16)
+    reqs[1].block_table = reqs[0].block_table[:2] + reqs[1].block_table[2:]
+    sess, step, q, out, lse = run_attn(sh, reqs, n, 21, attn_kernel=kernel, split_tiles=1)
+    # (run_attn wrote the shared pages for each request: what is there now)
+    K = pages_kv(sess, reqs)
+    k, v = rand(gen(1), 5, 2, 128), rand(gen(2), 5, 2, 128)
+    q_out = torch.empty_like(q)
+    sess.step_append(step, q, k, v, q_out)
+    lse = torch.empty(5, 8, device="cuda")
+    out = q_out.clone()
+    sess.step_attn(step, out, out, lse)
+    torch.cuda.synchronize()
+    check_attn(reqs, q_out, out, lse, K, 128, 70, part=part_of(step))
+
+
 def test_captured_step_replays():
     """append + attention captured in a graph, replayed on new inputs with
     eager work between the replays."""
@@ -715,7 +735,7 @@ def test_calls_refused_before_any_launch():
         bad("NULL", at, *a)
     bad("aligned", ap, own, q.data_ptr() + 8, k, k, rk, rv, None, q)
     bad("aligned", at, own, q, rk.data_ptr() + 2, rv, None, q.clone())
-    bad("aligned", at, own, q, rk, rv, None, q.clone(), 4100)
+    bad("aligned", at, own, q, rk, rv, None, q.clone(), 4098)
     bad("strides", ap, own, q, k, k, rk, rv, None, q.clone(), q_stride=1016)
     bad("strides", ap, own, q, k, k, rk, rv, None, q.clone(), k_stride=260)
     bad("strides", ap, own, q, k, k, rk, rv, None, q.clone(), v_stride=-256)
