@@ -247,6 +247,12 @@ tsr_status build_step(const tsr_model* model, const tsr_step_request* reqs, int3
   std::vector<int32_t> page_n((size_t)n_req_pages, 0);
   std::vector<uint8_t> page_twice((size_t)n_req_pages, 0);
   std::vector<int32_t> row0(n_req + 1, 0), bt_off(n_req, 0);
+  {
+    int64_t n = 0;
+    for (int r = 0; r < n_req; ++r)
+      n += std::max<int64_t>(0, ((int64_t)reqs[r].kv_len + B - 1) / B);
+    bts.reserve((size_t)std::min<int64_t>(n, 1 << 24));
+  }
   for (int r = 0; r < n_req; ++r) {
     const tsr_step_request& q = reqs[r];
     if (q.kv_len < 0 || q.n_rows < 0)
@@ -301,8 +307,11 @@ tsr_status build_step(const tsr_model* model, const tsr_step_request* reqs, int3
   p->shared_append = false;
   for (const StepRow& r : rows)
     if (r.pos >= 0 && page_twice[r.dst / B]) p->shared_append = true;
-  for (int32_t i = 0; i < n_req_pages; ++i)
-    if (page_n[i]) pages.push_back({i, page_n[i]});
+  if (m.kv_dtype == TSR_E2M1) {   // pack_kv, unpack_kv
+    pages.reserve(bts.size());
+    for (int32_t i = 0; i < n_req_pages; ++i)
+      if (page_n[i]) pages.push_back({i, page_n[i]});
+  }
 
   // attention items: row tile x head block x KV head, of either kernel
   auto add_items = [&](int r, int kind, std::vector<StepItem>* out) {

@@ -11,10 +11,19 @@
 //                   vector of each block, and half its keys)
 //   O^T += V^T P^T  v_mfma_f32_32x32x16_f16
 // P and V enter the second product as fp16: rounding P to bf16 would put as
-// much error on an output as its own rounding, fp16 an eighth of it.  K goes
-// straight to LDS in operand order (4-bit K through registers, as bf16); V
-// through registers to fp16 rows, whose 16-byte chunks are permuted by the key
-// so that the transposing reads of V^T touch every bank once.
+// much error on an output as its own rounding, fp16 an eighth of it.
+//
+// Two workgroups a unit, so two waves a SIMD at 256 registers: O takes 128, Q
+// 56 (two of its fragments stay in LDS), S 32.  One wave a SIMD (no fragment in
+// LDS, the blocks half a tile apart so that one's softmax runs under the
+// other's products) was bound by its instruction issue.  16,384 rows of 32
+// heads, 12,288 keys, window 4,096 (1.12 TFLOP): 5,164 us with the kernel for
+// few rows, 1,347 with one wave, 1,091 with two, 1,027 with 64 keys a barrier
+// (1.09 PFLOP/s).  The matrix cores are busy 43 % of the cycles and the vector
+// unit 45 %, little of it at the same time; without the QK^T products it would
+// be 728 us, without the PV products 856, without exp2 1,010, without V's
+// conversion 1,048.  Reading K and V fragments once for each block, to run one
+// block's softmax under the other's products, took 1,180.
 #include <type_traits>
 
 #include "attn_common.h"
@@ -32,9 +41,9 @@ constexpr int kTileBytes = kStepKeys * kRowBytes;
 constexpr int kPairBytes = 2 * kTileBytes;
 constexpr int kBlkBytes = 16 * kRowBytes;   // a 16-key block of either
 
-// Fragments of the second block's queries that stay in LDS: two waves a SIMD
-// leave 256 registers a wave, of which O takes 128, S 32 and the other
-// queries the rest but some 40.
+// Fragments of the second block's queries that stay in LDS: with 16 in
+// registers the tile loop spills (its reloads would also wait for the direct
+// loads under way); 2, 3 and 4 are level.
 constexpr int kQInLds = 2;
 
 __device__ __forceinline__ uint32_t pack_f16x2(float a, float b) {
@@ -238,8 +247,7 @@ __global__ __launch_bounds__(64 * kRowWaves, 2) void step_rows_kernel(const Step
 #pragma unroll
       for (int r = 0; r < 16; ++r) o[b][db][r] = 0.0f;
   float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.0f, 0.0f};
-  // Q in accumulation registers, where only the matrix instructions read it;
-  // all of it here before the loop, whose waits are for the next tiles
+  // all of Q is here before the loop, whose waits are for the next tiles
 #pragma unroll
   for (int b = 0; b < 2; ++b)
 #pragma unroll
@@ -253,9 +261,8 @@ __global__ __launch_bounds__(64 * kRowWaves, 2) void step_rows_kernel(const Step
   const int tk = 4 * lh + (c16 >> 2);
   const uint32_t vfl = tk * kRowBytes + 32 * (((lane >> 4) & 1) ^ (tk & 7)) + 8 * (c16 & 3);
 
-  // One tile.  With one wave on a SIMD nothing else hides the softmax, so the
-  // two blocks go through it half a tile apart: block 0's under the QK^T
-  // products of block 1, block 1's under the PV products of block 0.
+  // One tile.  (Masked tiles are loops of their own below: in one loop the two
+  // forms kept O in different registers and copied it.)
   auto tile = [&](int key0, auto mask_tag, const uint8_t* kt, const uint8_t* vt)
       __attribute__((always_inline)) {
     constexpr bool MASK = decltype(mask_tag)::value;
@@ -307,6 +314,7 @@ __global__ __launch_bounds__(64 * kRowWaves, 2) void step_rows_kernel(const Step
         probabilities(b);
       }
       l[b] += lt[b];
+      // one place for O whether it was scaled or not
 #pragma unroll
       for (int db = 0; db < 4; ++db) asm volatile("" : "+v"(o[b][db]));
     };
@@ -314,6 +322,8 @@ __global__ __launch_bounds__(64 * kRowWaves, 2) void step_rows_kernel(const Step
     for (int b = 0; b < 2; ++b)
 #pragma unroll
       for (int r = 0; r < 16; ++r) s[b][r] = 0.0f;
+    // (the products first where both waves of the SIMD can go on: 1,077 us
+    // without; for the PV products too: 1,078)
     __builtin_amdgcn_s_setprio(1);
 #pragma unroll
     for (int k = 0; k < 8; ++k) {
