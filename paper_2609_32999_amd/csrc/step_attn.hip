@@ -15,9 +15,9 @@
 // A token of 64 requests of 1,000 to 16,000 keys, window 4,096, 32 / 8 heads of
 // 128: 144 us, 5.3 TB/s of the pages it needs; of 16 requests of 8,000 to
 // 33,000 keys, 64 / 8 heads: 219 us, 5.3 TB/s (a large copy on the same card:
-// 4.5 to 5.2).  Over 4-bit pages 32 requests of 8,000 to 33,000 keys: 150 us,
-// 4.4 TB/s; there a tile takes 207 vector instructions for its 4.4 KB, and one
-// workgroup a unit instead of three ran 239 us.
+// 4.5 to 5.2).  Over 4-bit pages 32 requests of 8,000 to 33,000 keys: 141 to 150
+// us, 4.4 to 4.7 TB/s; there a tile takes 194 vector instructions for its 4.4
+// KB, and one workgroup a unit instead of three ran 239 us.
 #include <cmath>
 
 #include "attn_common.h"
@@ -32,7 +32,8 @@ namespace {
 // ------------------------------------------------ bf16 and 4-bit pages
 // A wave takes every fourth 32-key tile of the item's range and works alone
 // until the four join at the end: its tiles arrive in LDS by direct loads,
-// the next one under way while one is computed, and nothing but its own counter is waited for.
+// the next one under way while one is computed, and only its own counter is
+// waited for.
 //   S^T = K Q^T     16x16x32, two 16-key blocks: lane l holds query vector
 //                   l % 16 and keys 4 (l / 16) + 0 .. 3 of each block
 //   O^T += V^T P^T  16x16x32: those eight keys are the lane's operand, so P

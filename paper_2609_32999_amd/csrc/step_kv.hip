@@ -64,7 +64,7 @@ __device__ __forceinline__ void put8(uint16_t* p, const float* x) {
 // Bound by HBM.  A vector a group, and as many groups as there are vectors:
 // several vectors a group, to read the row's cos and sin once, left fewer
 // loads in flight (14,892 rows, 32 + 16 heads of 128: 77 us, 5.3 TB/s, with
-// one; 80, 84, 88 and 92 with 2, 3, 4 and 6).
+// one, 73 on another card; 80, 84, 88 and 92 with 2, 3, 4 and 6).
 template <typename E, int KIND, int D>
 __global__ __launch_bounds__(256) void step_append_kernel(const AppendArgs a) {
   constexpr int L = D / 16, H = D / 2;

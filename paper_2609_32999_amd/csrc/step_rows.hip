@@ -18,12 +18,13 @@
 // LDS, the blocks half a tile apart so that one's softmax runs under the
 // other's products) was bound by its instruction issue.  16,384 rows of 32
 // heads, 12,288 keys, window 4,096 (1.12 TFLOP): 5,164 us with the kernel for
-// few rows, 1,347 with one wave, 1,091 with two, 1,027 with 64 keys a barrier
-// (1.09 PFLOP/s).  The matrix cores are busy 43 % of the cycles and the vector
-// unit 45 %, little of it at the same time; without the QK^T products it would
-// be 728 us, without the PV products 856, without exp2 1,010, without V's
-// conversion 1,048.  Reading K and V fragments once for each block, to run one
-// block's softmax under the other's products, took 1,180.
+// few rows, 1,347 with one wave, 1,091 with two, 986 to 1,030 (by the card's
+// clock) with 64 keys a barrier: 1.08 to 1.13 PFLOP/s, where a large library
+// product reaches 1.39.  The matrix cores are busy 55 % of the cycles and the
+// vector unit 54 %, much of it in turn: of 1,080 us, 728 were left without the
+// QK^T products, 856 without the PV products, 1,010 without exp2, 1,048
+// without V's conversion.  Reading K and V fragments once for each block, to
+// run one block's softmax under the other's products, took 1,180.
 #include <type_traits>
 
 #include "attn_common.h"
