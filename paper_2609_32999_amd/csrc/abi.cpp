@@ -7,7 +7,6 @@
 #include <exception>
 #include <new>
 #include <string>
-#include <system_error>
 #include <thread>
 #include <vector>
 
@@ -275,7 +274,7 @@ tsr_status tsr_rope_table_init(const tsr_model* model, void* dev_table,
     for (int t = 1; t < parts; ++t) {
       try {
         threads.emplace_back(fill, first(t), first(t + 1));
-      } catch (const std::system_error&) {   // no thread to be had: here, then
+      } catch (const std::exception&) {   // no thread to be had: here, then
         fill(first(t), first(t + 1));
       }
     }
