@@ -725,6 +725,15 @@ class StepBatch:
                 self._keep.append(a)
                 ptrs.append(_i32p(a))
             self.array[i] = tsr_step_request(int(r.kv_len), int(r.n_rows), *ptrs)
+        self._held = [(int(r.kv_len), len(r.block_table)) for r in requests
+                      if getattr(r, "block_table", None) is not None]
+
+    def check_tables(self, page_size: int) -> None:
+        """The library reads ceil(kv_len / page_size) entries of a block table."""
+        for kv_len, n in self._held:
+            if n * page_size < kv_len:
+                raise ValueError(f"a block table of {n} pages of {page_size} does not hold "
+                                 f"kv_len {kv_len}")
 
 
 def _step_options(window: int, n_sinks: int, split_tiles: int, attn_kernel: int):

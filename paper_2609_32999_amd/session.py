@@ -242,6 +242,7 @@ class Session:
             raise ValueError("the session was made without four_bit=True")
         model = self.model4 if four_bit else self.model
         batch = B.StepBatch(requests)
+        batch.check_tables(self.shape.page_size)
         opts = dict(window=window, n_sinks=n_sinks, split_tiles=split_tiles,
                     attn_kernel=attn_kernel)
         n = B.tsr_step_workspace_size(model, batch, self.n_req_pages, **opts)
@@ -268,7 +269,11 @@ class Session:
                              f"{self.act_dtype} on {self.req_k.device}")
         if step.num_rows and (x.stride(2) != 1 or (heads > 1 and x.stride(1) != d)):
             raise ValueError(f"{what}: the heads of a row must be contiguous")
-        return x.stride(0) if step.num_rows > 1 else 0
+        if step.num_rows < 2:
+            return 0
+        if x.stride(0) < heads * d:   # an expanded row: 0 means packed to the library
+            raise ValueError(f"{what}: rows must not overlap")
+        return x.stride(0)
 
     def step_append(self, step, q, k, v, q_out, k_pre=None, q_weight=None, k_weight=None,
                     eps: float | None = None, layer: int = 0, stream=None):

@@ -213,3 +213,27 @@ def test_step_of_a_plan_row_set():
             for i, q in enumerate(wl.requests)]
     assert make(reqs, m, wl.n_req_pages).num_rows == plan.num_compute_tokens
     assert np.any(lo > 0)
+
+
+def test_batch_checks_block_tables():
+    from paper_2609_32999_amd.session import Session
+    reqs = [req(), req(kv_len=33, table=[3, 4])]
+    b = P.StepBatch(reqs)
+    with pytest.raises(ValueError, match="does not hold kv_len 33"):
+        b.check_tables(16)
+    b.check_tables(32)   # 64 slots hold 33
+    with pytest.raises(ValueError, match="does not hold kv_len 33"):
+        Session.step(NS(shape=NS(page_size=16), model=model()), reqs)
+
+
+def test_session_refuses_overlapping_rows():
+    torch = pytest.importorskip("torch")
+    from paper_2609_32999_amd.session import Session
+    sess = NS(shape=NS(head_dim=128), act_dtype=torch.bfloat16, req_k=torch.empty(0))
+    step = NS(num_rows=3)
+    fused = torch.zeros(3, 4 * 128 + 64, dtype=torch.bfloat16)
+    rows = fused[:, :4 * 128].unflatten(1, (4, 128))
+    assert Session._rows(sess, step, rows, 4, "q") == 4 * 128 + 64
+    with pytest.raises(ValueError, match="overlap"):
+        Session._rows(sess, step, rows[:1].expand(3, 4, 128), 4, "q")
+    assert Session._rows(sess, NS(num_rows=1), rows[:1], 4, "q") == 0
