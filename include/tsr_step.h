@@ -123,7 +123,8 @@ size_t tsr_step_workspace_size(const tsr_model* model, const tsr_step_request* r
  * HIP call is made).  dev_rope_table: a table of tsr_rope_table_init for the
  * model.  Rows are in the order given: requests in order, and within a
  * request its rows in order.  A step is immutable and serves every layer of
- * the model. */
+ * the model.  Destroy it, or let its workspace go, only when the work that uses
+ * it is done; a captured graph of its calls needs both while it replays. */
 tsr_status tsr_step_create(const tsr_model* model, const tsr_step_request* reqs, int32_t n_req,
                            int32_t n_req_pages, const tsr_step_options* options,
                            const void* dev_rope_table, void* dev_workspace,
@@ -172,7 +173,8 @@ tsr_status tsr_step_append(const tsr_step* step, const tsr_qk_norm* norm, const 
  * bound by reading the pages) the probabilities enter the second product as
  * two bf16 parts.  For many (256 an item, bound by the matrix cores) they and
  * the values enter it as fp16: a value beyond 65504 in magnitude makes the
- * outputs that see it non-finite.  With attn_kernel 0 each request goes to
+ * outputs that see it non-finite, and values below 2^-14 keep an absolute
+ * accuracy of 2^-25. With attn_kernel 0 each request goes to
  * the one its rows are sooner done with.  Results do not depend on the order
  * in which the launch runs; they differ in rounding between the kernels and
  * between key ranges. */

@@ -20,6 +20,10 @@ constexpr int kStepRowVecs = 256;
 // Keys per tile: two 16-key blocks, each within one page (bf16, e2m1).
 constexpr int kStepKeys = 32;
 
+// Workgroups of a launch: 256 threads each, and HIP takes fewer than 2^32
+// threads.
+constexpr int64_t kMaxBlocks = ((int64_t)1 << 24) - 1;
+
 // A row: its position (-1: no token), first visible key and, as an append
 // target, the slot page * page_size + slot-in-page of its position.
 struct alignas(16) StepRow {

@@ -340,6 +340,12 @@ tsr_status build_step(const tsr_model* model, const tsr_step_request* reqs, int3
           out->push_back(it);
         }
   };
+  int64_t least = 0;   // items if all were the second kernel's
+  for (int r = 0; r < n_req; ++r) {
+    const int rt = kStepRowVecs / G;
+    least += (int64_t)Hkv * ((row0[r + 1] - row0[r] + rt - 1) / rt);
+  }
+  if (least > kMaxBlocks) return fail(TSR_ERR_OUT_OF_RANGE, "too many attention items");
   std::vector<StepItem> whole[2];
   std::vector<int> either;   // requests that both kernels may serve
   for (int r = 0; r < n_req; ++r) {
@@ -392,7 +398,7 @@ tsr_status build_step(const tsr_model* model, const tsr_step_request* reqs, int3
       else
         whole[0].insert(whole[0].end(), few[i].begin(), few[i].end());
   }
-  if (whole[0].size() + whole[1].size() > (size_t)INT32_MAX / 64)
+  if (whole[0].size() + whole[1].size() > (size_t)kMaxBlocks)
     return fail(TSR_ERR_OUT_OF_RANGE, "too many attention items");
 
   // the page ids of an item's first tiles, one for each wave
@@ -445,6 +451,8 @@ tsr_status build_step(const tsr_model* model, const tsr_step_request* reqs, int3
     const size_t before = items.size();
     schedule(list, &items);
     p->n_items[kind] = (int32_t)(items.size() - before);
+    if (p->n_items[kind] > kMaxBlocks)
+      return fail(TSR_ERR_OUT_OF_RANGE, "too many attention items");
   }
   p->n_merges = (int32_t)merges.size();
   p->n_pages = (int32_t)pages.size();
@@ -629,6 +637,9 @@ tsr_status tsr_step_append(const tsr_step* p, const tsr_qk_norm* norm, const voi
                                          "bytes");
     }
     if (p->T == 0) return TSR_OK;
+    if (((int64_t)p->T * (m.n_q_heads + 2 * m.n_kv_heads) * (m.head_dim / 16) + 255) / 256 >
+        kMaxBlocks)
+      return fail(TSR_ERR_OUT_OF_RANGE, "too many rows for one append");
     if (!q || !k || !v || !q_out || !req_k || !req_v) return null_pointer("step_append");
     if (!aligned({q, k, v, q_out, k_pre, req_k, req_v, req_scale})) return misaligned();
     if ((q_out == q && q_stride != packed_q) || (k_pre == k && k_stride != packed_kv))
@@ -668,6 +679,8 @@ tsr_status tsr_step_pack_kv(const tsr_step* p, const void* bf16_k, const void* b
     if (!is_e2m1(p))
       return fail(TSR_ERR_INVALID_ARG, "pack_kv applies to steps of a 4-bit (E2M1) model");
     if (p->n_pages == 0) return TSR_OK;
+    if (p->n_pages > kMaxBlocks)
+      return fail(TSR_ERR_OUT_OF_RANGE, "too many pages for one call");
     if (!bf16_k || !bf16_v || !req_k || !req_v || !req_scale) return null_pointer("step_pack_kv");
     if (!aligned({bf16_k, bf16_v, req_k, req_v, req_scale})) return misaligned();
     hipError_t e = launch_step_pack(p, bf16_k, bf16_v, req_k, req_v, req_scale,
@@ -685,6 +698,8 @@ tsr_status tsr_step_unpack_kv(const tsr_step* p, const void* req_k, const void* 
     if (!is_e2m1(p))
       return fail(TSR_ERR_INVALID_ARG, "unpack_kv applies to steps of a 4-bit (E2M1) model");
     if (p->n_pages == 0) return TSR_OK;
+    if (p->n_pages > kMaxBlocks)
+      return fail(TSR_ERR_OUT_OF_RANGE, "too many pages for one call");
     if (!bf16_k || !bf16_v || !req_k || !req_v || !req_scale)
       return null_pointer("step_unpack_kv");
     if (!aligned({bf16_k, bf16_v, req_k, req_v, req_scale})) return misaligned();

@@ -237,3 +237,9 @@ def test_session_refuses_overlapping_rows():
     with pytest.raises(ValueError, match="overlap"):
         Session._rows(sess, step, rows[:1].expand(3, 4, 128), 4, "q")
     assert Session._rows(sess, NS(num_rows=1), rows[:1], 4, "q") == 0
+
+
+def test_launch_limit():
+    # a work item for each row and KV head: 2^24 and more of them
+    reqs = [req(kv_len=1, first=0)] * 4096
+    refused(P.TSR_ERR_OUT_OF_RANGE, "too many attention items", reqs=reqs, m=model(4096, 4096))
