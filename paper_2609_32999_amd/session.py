@@ -237,7 +237,11 @@ class Session:
         """Validate and upload a step: rows of requests whose KV is in request
         pages (objects with kv_len, n_rows, block_table, and optionally
         positions and row_lo).  `four_bit`: over the 4-bit arena.  `window`
-        and `n_sinks` are its attention's sliding window and sinks."""
+        and `n_sinks` are its attention's sliding window and sinks.
+
+        The workspace belongs to `stream`: work of the step on another stream
+        has to be done, or waited for by `stream`, before the step is dropped,
+        and a captured graph of its calls needs it for as long as it replays."""
         if four_bit and self.req4_k is None:
             raise ValueError("the session was made without four_bit=True")
         model = self.model4 if four_bit else self.model
@@ -246,9 +250,13 @@ class Session:
         opts = dict(window=window, n_sinks=n_sinks, split_tiles=split_tiles,
                     attn_kernel=attn_kernel)
         n = B.tsr_step_workspace_size(model, batch, self.n_req_pages, **opts)
-        ws = torch.empty(n, dtype=torch.uint8, device=self.device)
-        step = B.tsr_step_create(model, batch, self.n_req_pages, self.rope, ws, n,
-                                 stream or self.stream, **opts)
+        s = stream or self.stream
+        # allocated on the stream that fills it: memory that another stream's
+        # work was done with would not be free for this one yet
+        with torch.cuda.stream(s if isinstance(s, torch.cuda.Stream) else
+                               torch.cuda.ExternalStream(s, self.device)):
+            ws = torch.empty(n, dtype=torch.uint8, device=self.device)
+        step = B.tsr_step_create(model, batch, self.n_req_pages, self.rope, ws, n, s, **opts)
         step.workspace = ws     # keep the workspace alive with the step
         step.batch = batch
         step.four_bit = four_bit

@@ -476,6 +476,28 @@ def test_pack_and_unpack(page, hkv):
         np.testing.assert_array_equal(f64(back[0]), want.astype(np.float32))
 
 
+def test_unpack_any_codes_and_scales():
+    """Pages that others wrote: all 16 codes under all 256 scale bytes."""
+    sh = shape(2, 2)
+    reqs, n = batch([(64, 1)], 16)
+    sess = Session(sh, 1, n, four_bit=True)
+    g = gen(5)
+    for c in (sess.req4_k, sess.req4_v):
+        c.copy_(torch.randint(0, 256, c.shape, generator=g, dtype=torch.uint8))
+    # 256 scales a page, half of them K's: every byte of either in two pages
+    for i, pg in enumerate(reqs[0].block_table):
+        sess.req4_scale[0, pg] = (torch.arange(256).roll(128 * i).to(torch.uint8)
+                                  .reshape(sess.req4_scale.shape[2:]).cuda())
+    sess.unpack_step(sess.step(reqs, four_bit=True))
+    torch.cuda.synchronize()
+    t = torch.tensor(reqs[0].block_table)
+    for w, (back, codes) in enumerate(((sess.req_k, sess.req4_k), (sess.req_v, sess.req4_v))):
+        want = O.e2m1_decode(codes[0][t].cpu().numpy(), sess.req4_scale[0][t, w].cpu().numpy())
+        with np.errstate(over="ignore"):
+            want = want.astype(np.float32)   # past fp32: infinite in bf16 too
+        np.testing.assert_array_equal(f64(back[0][t]), want)
+
+
 def test_append_to_four_bit_pages():
     sess, step, reqs, q, k, v, wq, wk = append_case("bf16", 8, 2, 128, 16, True, four_bit=True)
     T = step.num_rows
@@ -699,6 +721,29 @@ def test_one_step_on_two_streams():
     torch.cuda.synchronize()
     for o in outs:
         assert torch.equal(o, out)
+
+
+@pytest.mark.parametrize("handle", [False, True])
+def test_step_of_a_stream(handle):
+    """A step made for a stream other than the current one, between other work
+    on either, with its workspace in memory freed on the current one."""
+    sh = shape(8, 2)
+    reqs, n = batch([(700, 1), (90, 1)], 16)
+    sess, step, q, out, lse = run_attn(sh, reqs, n, 21, split_tiles=2)
+    assert step.num_attn_splits > 0
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    for i in range(3):
+        junk = torch.full((step.workspace.numel(),), i, dtype=torch.uint8, device="cuda")
+        for _ in range(20):
+            junk.add_(1)
+        del junk   # free for the current stream only
+        other = sess.step(reqs, stream=side.cuda_stream if handle else side, split_tiles=2)
+        o, l = torch.empty_like(out), torch.empty_like(lse)
+        side.wait_stream(torch.cuda.current_stream())
+        sess.step_attn(other, q, o, l, stream=side)
+        torch.cuda.synchronize()
+        assert torch.equal(o, out) and torch.equal(l, lse)
 
 
 # ---------------------------------------------------------------- refusals
