@@ -3,9 +3,14 @@
 //
 // Bound by the matrix cores, and before them by LDS: a K or V fragment read
 // from LDS feeds one 32x32x16 product a block of 32 vectors (rows x heads), 32
-// cycles of a SIMD for 1 KB, and four SIMDs share 128 bytes a cycle.  So a
-// wave owns two blocks, 64 vectors, and uses every fragment twice; a workgroup
-// of four waves, 256 vectors, stages each 32-key tile once for all of them.
+// cycles of a SIMD for 1 KB, and four SIMDs share 128 bytes a cycle.  A
+// workgroup takes 256 vectors and stages each 32-key tile once for all of them:
+//   - four waves of two blocks use every fragment twice; two workgroups share a
+//     unit, 64 keys a barrier each;
+//   - eight waves of one block, 128 keys a barrier, in a launch that leaves a
+//     workgroup a unit of its own: two waves of it take turns on each SIMD (256
+//     items of 2,048 keys: 90 us instead of 105, 4-bit 88 instead of 109; two
+//     for each unit: 173 and 157, 4-bit 165 and 159).
 //   S^T = K Q^T     v_mfma_f32_32x32x16_bf16
 //   online softmax  fp32, lane-local but for one exchange (a lane holds one
 //                   vector of each block, and half its keys)
@@ -13,8 +18,9 @@
 // P and V enter the second product as fp16: rounding P to bf16 would put as
 // much error on an output as its own rounding, fp16 an eighth of it.
 //
-// Two workgroups a unit, so two waves a SIMD at 256 registers: O takes 128, Q
-// 56 (two of its fragments stay in LDS), S 32.  One wave a SIMD (no fragment in
+// Either way two waves a SIMD, at 256 registers: of two blocks, O takes 128, Q
+// 56 (two of its fragments stay in LDS), S 32.  (One block at 128 registers and
+// four waves spills: 1,571 us below.)  One wave a SIMD (no fragment in
 // LDS, the blocks half a tile apart so that one's softmax runs under the
 // other's products) was bound by its instruction issue.  16,384 rows of 32
 // heads, 12,288 keys, window 4,096 (1.12 TFLOP): 5,164 us with the kernel for
@@ -36,16 +42,14 @@ namespace tsr {
 
 namespace {
 
-constexpr int kRowWaves = 4;
 constexpr int kRowBytes = 2 * kD;   // a key's K or V row in LDS
 constexpr int kTileBytes = kStepKeys * kRowBytes;
-constexpr int kPairBytes = 2 * kTileBytes;
 constexpr int kBlkBytes = 16 * kRowBytes;   // a 16-key block of either
 
-// Fragments of the second block's queries that stay in LDS: with 16 in
+// Fragments of a second block's queries that stay in LDS: with 16 in
 // registers the tile loop spills (its reloads would also wait for the direct
 // loads under way); 2, 3 and 4 are level.
-constexpr int kQInLds = 2;
+template <int NB> constexpr int kQInLds = NB == 2 ? 2 : 0;
 
 __device__ __forceinline__ uint32_t pack_f16x2(float a, float b) {
   const f16x2 h = {(_Float16)a, (_Float16)b};
@@ -65,14 +69,17 @@ __device__ __forceinline__ uint32_t finite_or_0(uint32_t w) {
   return w & ~(off * 0xffffu);
 }
 
-template <bool F4>
-__global__ __launch_bounds__(64 * kRowWaves, 2) void step_rows_kernel(const StepAttnArgs a) {
-  // two pairs of tiles, K and V
-  __shared__ __attribute__((aligned(1024))) uint8_t kl[2 * kPairBytes];
-  __shared__ __attribute__((aligned(1024))) uint8_t vl[2 * kPairBytes];
+// NB: blocks of 32 vectors a wave.
+template <bool F4, int NB>
+__global__ __launch_bounds__(512 / NB, 2) void step_rows_kernel(const StepAttnArgs a) {
+  constexpr int NW = 8 / NB, TG = NW / 2, QL = kQInLds<NB>;
+  constexpr int kGroupBytes = TG * kTileBytes;
+  // two groups of tiles, K and V
+  __shared__ __attribute__((aligned(1024))) uint8_t kl[2 * kGroupBytes];
+  __shared__ __attribute__((aligned(1024))) uint8_t vl[2 * kGroupBytes];
   __shared__ Sight sights[kStepRowVecs];
-  __shared__ __attribute__((aligned(16))) uint4 q_lds[kRowWaves][kQInLds][64];
-  __shared__ uint32_t bad_v[kRowWaves];   // wave w replaced values that are not finite
+  __shared__ __attribute__((aligned(16))) uint4 q_lds[NW][QL > 0 ? QL : 1][64];
+  __shared__ uint32_t bad_v[NW];   // wave w replaced values that are not finite
 
   const StepItem it = a.items[blockIdx.x];
   if (it.n_rows == 0) return;
@@ -87,8 +94,8 @@ __global__ __launch_bounds__(64 * kRowWaves, 2) void step_rows_kernel(const Step
   auto tile_key = [&](int t) { return kStepKeys * (t < na ? it.a0 + t : it.b0 + t - na); };
   const int last = it.kv_len - 1, last_blk = last & ~15;
 
-  // ---- staging, a pair of tiles ahead: wave w brings 16-key block w of the
-  // pair, K and V, by direct loads.
+  // ---- staging, a group of TG tiles ahead: wave w brings 16-key block w of the
+  // group, K and V, by direct loads.
   //   bf16   K in operand order; V as rows with their chunks permuted, which
   //          its wave turns into fp16 in place once they are there;
   //   4-bit  codes and scales to the front of the block's space in either
@@ -111,8 +118,8 @@ __global__ __launch_bounds__(64 * kRowWaves, 2) void step_rows_kernel(const Step
   auto issue = [&](int t, int slot) __attribute__((always_inline)) {
     const int kb = my_key(t), top = last - kb;
     const uint64_t key = (uint64_t)(uint32_t)page * page_keys + head_key + (kb & page_mask);
-    const uint32_t kd = lds_addr(kl) + slot * kPairBytes + w * kBlkBytes;
-    const uint32_t vd = lds_addr(vl) + slot * kPairBytes + w * kBlkBytes;
+    const uint32_t kd = lds_addr(kl) + slot * kGroupBytes + w * kBlkBytes;
+    const uint32_t vd = lds_addr(vl) + slot * kGroupBytes + w * kBlkBytes;
     const int lane = lane_now(), c16 = lane & 15, c4 = lane >> 4;
     const int kk = min(c16, top);
     if constexpr (!F4) {
@@ -158,8 +165,8 @@ __global__ __launch_bounds__(64 * kRowWaves, 2) void step_rows_kernel(const Step
   auto convert = [&](int t, int slot) __attribute__((always_inline)) {
     const int key0 = tile_key(min(t + (w >> 1), nt - 1));
     const bool masked = key0 < it.full_lo || key0 + kStepKeys - 1 > it.full_hi;
-    uint8_t* kt = kl + slot * kPairBytes + w * kBlkBytes;
-    uint8_t* vt = vl + slot * kPairBytes + w * kBlkBytes;
+    uint8_t* kt = kl + slot * kGroupBytes + w * kBlkBytes;
+    uint8_t* vt = vl + slot * kGroupBytes + w * kBlkBytes;
     const int lane = lane_now(), c16 = lane & 15, c4 = lane >> 4;
     uint4 x[4];
     if constexpr (!F4) {
@@ -192,22 +199,22 @@ __global__ __launch_bounds__(64 * kRowWaves, 2) void step_rows_kernel(const Step
     }
   };
 
-  if (tid < kRowWaves) bad_v[tid] = 0;
+  if (tid < NW) bad_v[tid] = 0;
   if (nt > 0) {
     fetch_page(0);
     issue(0, 0);
   }
-  if (nt > 2) fetch_page(2);
+  if (nt > TG) fetch_page(TG);
 
-  // ---- this wave's vectors: v = 64 w + 32 b + l32 is row v / heads, head v %
+  // ---- this wave's vectors: v = 32 NB w + 32 b + l32 is row v / heads, head v %
   // heads of the item; vectors past the last repeat the last row
-  Frag qf[2][8];
+  Frag qf[NB][8];
   // keys [seen_lo, seen_hi] hold all that the wave's rows see beside the sinks,
   // which end at sink_hi
   int seen_lo = INT32_MAX, seen_hi = -1, sink_hi = 0;
 #pragma unroll
-  for (int b = 0; b < 2; ++b) {
-    const int v = 64 * w + 32 * b + l32;
+  for (int b = 0; b < NB; ++b) {
+    const int v = 32 * (NB * w + b) + l32;
     int r = v / it.n_heads, h = v - r * it.n_heads;
     if (r >= it.n_rows) {
       r = it.n_rows - 1;
@@ -238,23 +245,25 @@ __global__ __launch_bounds__(64 * kRowWaves, 2) void step_rows_kernel(const Step
   seen_lo = __builtin_amdgcn_readfirstlane(seen_lo);
   seen_hi = __builtin_amdgcn_readfirstlane(seen_hi);
   sink_hi = __builtin_amdgcn_readfirstlane(sink_hi);
-  const bool active = 64 * w < it.n_rows * it.n_heads;
+  const bool active = 32 * NB * w < it.n_rows * it.n_heads;
 
-  f32x16 o[2][4];
+  f32x16 o[NB][4];
 #pragma unroll
-  for (int b = 0; b < 2; ++b)
+  for (int b = 0; b < NB; ++b)
 #pragma unroll
     for (int db = 0; db < 4; ++db)
 #pragma unroll
       for (int r = 0; r < 16; ++r) o[b][db][r] = 0.0f;
-  float m[2] = {-INFINITY, -INFINITY}, l[2] = {0.0f, 0.0f};
+  float m[NB], l[NB];
+#pragma unroll
+  for (int b = 0; b < NB; ++b) m[b] = -INFINITY, l[b] = 0.0f;
   // all of Q is here before the loop, whose waits are for the next tiles
 #pragma unroll
-  for (int b = 0; b < 2; ++b)
+  for (int b = 0; b < NB; ++b)
 #pragma unroll
     for (int k = 0; k < 8; ++k) asm volatile("" : "+v"(qf[b][k].b));
 #pragma unroll
-  for (int k = 0; k < kQInLds; ++k) q_lds[w][k][lane] = qf[1][8 - kQInLds + k].u;
+  for (int k = 0; k < QL; ++k) q_lds[w][k][lane] = qf[NB - 1][8 - QL + k].u;
   const float sc = a.scale_log2e;
   // operand reads: K fragment k at kfl + (k / 2) 1024 + (k % 2) 512; V^T
   // fragment (16 keys h, 32 dims db) at (vfl ^ 64 db) + 4096 h, + 2048
@@ -267,9 +276,9 @@ __global__ __launch_bounds__(64 * kRowWaves, 2) void step_rows_kernel(const Step
   auto tile = [&](int key0, auto mask_tag, const uint8_t* kt, const uint8_t* vt)
       __attribute__((always_inline)) {
     constexpr bool MASK = decltype(mask_tag)::value;
-    f32x16 s[2];
-    uint32_t pw[2][8];   // P as fp16 pairs
-    float lt[2];
+    f32x16 s[NB];
+    uint32_t pw[NB][8];   // P as fp16 pairs
+    float lt[NB];
     auto probabilities = [&](int b) __attribute__((always_inline)) {
       const float mc = m[b] == -INFINITY ? 0.0f : m[b] * sc;
       float ls[2] = {0.0f, 0.0f};
@@ -290,7 +299,7 @@ __global__ __launch_bounds__(64 * kRowWaves, 2) void step_rows_kernel(const Step
     };
     auto softmax = [&](int b) __attribute__((always_inline)) {
       if constexpr (MASK) {
-        const uint32_t bits = seen_bits(sights[64 * w + 32 * b + l32], key0) >> (4 * lh);
+        const uint32_t bits = seen_bits(sights[32 * (NB * w + b) + l32], key0) >> (4 * lh);
 #pragma unroll
         for (int r = 0; r < 16; ++r) s[b][r] = where_bit(bits, 8 * (r >> 2) + (r & 3), s[b][r]);
       }
@@ -320,7 +329,7 @@ __global__ __launch_bounds__(64 * kRowWaves, 2) void step_rows_kernel(const Step
       for (int db = 0; db < 4; ++db) asm volatile("" : "+v"(o[b][db]));
     };
 #pragma unroll
-    for (int b = 0; b < 2; ++b)
+    for (int b = 0; b < NB; ++b)
 #pragma unroll
       for (int r = 0; r < 16; ++r) s[b][r] = 0.0f;
     // (the products first where both waves of the SIMD can go on: 1,077 us
@@ -331,9 +340,11 @@ __global__ __launch_bounds__(64 * kRowWaves, 2) void step_rows_kernel(const Step
       Frag f;
       f.u = *reinterpret_cast<const uint4*>(kt + kfl + 1024 * (k >> 1) + 512 * (k & 1));
       s[0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f.b, qf[0][k].b, s[0], 0, 0, 0);
-      Frag q1 = qf[1][k];
-      if (k >= 8 - kQInLds) q1.u = q_lds[w][k - 8 + kQInLds][lane];
-      s[1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f.b, q1.b, s[1], 0, 0, 0);
+      if constexpr (NB == 2) {
+        Frag q1 = qf[1][k];
+        if (k >= 8 - QL) q1.u = q_lds[w][k - 8 + QL][lane];
+        s[1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f.b, q1.b, s[1], 0, 0, 0);
+      }
     }
     __builtin_amdgcn_s_setprio(0);
     // keep LDS reads in flight ahead of the products (scheduling groups: 0x100
@@ -341,17 +352,18 @@ __global__ __launch_bounds__(64 * kRowWaves, 2) void step_rows_kernel(const Step
     __builtin_amdgcn_sched_group_barrier(0x100, 5, 0);
 #pragma unroll
     for (int k = 0; k < 8; ++k) {
-      __builtin_amdgcn_sched_group_barrier(0x008, 2, 0);
+      __builtin_amdgcn_sched_group_barrier(0x008, NB, 0);
       __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
     }
     __builtin_amdgcn_sched_barrier(0);
-    softmax(0);
-    settle(0);
-    softmax(1);
-    settle(1);
-    Frag pf[2][2];
 #pragma unroll
-    for (int b = 0; b < 2; ++b)
+    for (int b = 0; b < NB; ++b) {
+      softmax(b);
+      settle(b);
+    }
+    Frag pf[NB][2];
+#pragma unroll
+    for (int b = 0; b < NB; ++b)
 #pragma unroll
       for (int h = 0; h < 2; ++h)
         pf[b][h].u = make_uint4(pw[b][4 * h], pw[b][4 * h + 1], pw[b][4 * h + 2], pw[b][4 * h + 3]);
@@ -365,13 +377,13 @@ __global__ __launch_bounds__(64 * kRowWaves, 2) void step_rows_kernel(const Step
         const uint2 y = lds_read_transposed((va ^ (64 * db)) + 4096 * h + 2048);
         f.u = make_uint4(x.x, x.y, y.x, y.y);
 #pragma unroll
-        for (int b = 0; b < 2; ++b)
+        for (int b = 0; b < NB; ++b)
           o[b][db] = __builtin_amdgcn_mfma_f32_32x32x16_f16(f.h, pf[b][h].h, o[b][db], 0, 0, 0);
       }
     __builtin_amdgcn_sched_group_barrier(0x100, 6, 0);
 #pragma unroll
     for (int k = 0; k < 8; ++k) {
-      __builtin_amdgcn_sched_group_barrier(0x008, 2, 0);
+      __builtin_amdgcn_sched_group_barrier(0x008, NB, 0);
       __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
     }
   };
@@ -382,16 +394,16 @@ __global__ __launch_bounds__(64 * kRowWaves, 2) void step_rows_kernel(const Step
   __syncthreads();
   auto run = [&](int p0, int p1, auto mask_tag) __attribute__((always_inline)) {
     for (int p = p0; p < p1; ++p) {
-      const int t = 2 * p, slot = p & 1;
-      if (t + 2 < nt) {
-        wait_lds();   // the pair before last has been read
-        issue(t + 2, slot ^ 1);
-        if (t + 4 < nt) fetch_page(t + 4);
+      const int t = TG * p, slot = p & 1;
+      if (t + TG < nt) {
+        wait_lds();   // the group before last has been read
+        issue(t + TG, slot ^ 1);
+        if (t + 2 * TG < nt) fetch_page(t + 2 * TG);
       }
 #pragma unroll
-      for (int e = 0; e < 2; ++e) {
-        const uint8_t* kt = kl + slot * kPairBytes + e * kTileBytes;
-        const uint8_t* vt = vl + slot * kPairBytes + e * kTileBytes;
+      for (int e = 0; e < TG; ++e) {
+        const uint8_t* kt = kl + slot * kGroupBytes + e * kTileBytes;
+        const uint8_t* vt = vl + slot * kGroupBytes + e * kTileBytes;
         if constexpr (decltype(mask_tag)::value) {
           if (t + e >= nt) break;
           const int key0 = tile_key(t + e);
@@ -401,9 +413,9 @@ __global__ __launch_bounds__(64 * kRowWaves, 2) void step_rows_kernel(const Step
           tile(0, mask_tag, kt, vt);
         }
       }
-      if (t + 2 < nt) {
+      if (t + TG < nt) {
         wait_vm<0>();
-        convert(t + 2, slot ^ 1);
+        convert(t + TG, slot ^ 1);
       }
       __syncthreads();
     }
@@ -411,14 +423,18 @@ __global__ __launch_bounds__(64 * kRowWaves, 2) void step_rows_kernel(const Step
   // tiles [f0, f1) are seen in full by every row of the item
   const int f0 = min(nt, na + max(0, (it.full_lo + kStepKeys - 1) / kStepKeys - it.b0));
   const int f1 = max(f0, min(nt, na + (it.full_hi + 1) / kStepKeys - it.b0));
-  const int n_pairs = (nt + 1) / 2, p0 = min(n_pairs, (f0 + 1) / 2), p1 = max(p0, f1 / 2);
+  const int n_groups = (nt + TG - 1) / TG;
+  const int p0 = min(n_groups, (f0 + TG - 1) / TG), p1 = max(p0, f1 / TG);
   run(0, p0, std::true_type{});
   run(p0, p1, std::false_type{});
-  run(p1, n_pairs, std::true_type{});
+  run(p1, n_groups, std::true_type{});
 
   if (!active) return;
   // ---- values that are not finite, for the rows that see them
-  if (bad_v[0] | bad_v[1] | bad_v[2] | bad_v[3]) {
+  uint32_t bad = 0;
+#pragma unroll
+  for (int i = 0; i < NW; ++i) bad |= bad_v[i];
+  if (bad) {
 #pragma unroll 1
     for (int t = 0; t < nt; ++t) {
       const int key0 = tile_key(t);
@@ -429,7 +445,9 @@ __global__ __launch_bounds__(64 * kRowWaves, 2) void step_rows_kernel(const Step
         const int64_t slot = ((page * a.n_kv_heads + it.kv_head) << a.log2_page) + (j & page_mask);
         const int64_t scale = ((((2 * page + 1) * a.n_kv_heads + it.kv_head) << a.log2_page) +
                                (j & page_mask)) * (kD / kScaleDims);
-        const bool see[2] = {sees(sights[64 * w + l32], j), sees(sights[64 * w + 32 + l32], j)};
+        bool see[NB];
+#pragma unroll
+        for (int b = 0; b < NB; ++b) see[b] = sees(sights[32 * (NB * w + b) + l32], j);
 #pragma unroll
         for (int db = 0; db < 4; ++db)
 #pragma unroll
@@ -450,7 +468,7 @@ __global__ __launch_bounds__(64 * kRowWaves, 2) void step_rows_kernel(const Step
               const float y = (float)__builtin_bit_cast(f16x2, f[e >> 1])[e & 1];
               if (fabsf(y) <= 65504.0f) continue;
 #pragma unroll
-              for (int b = 0; b < 2; ++b)
+              for (int b = 0; b < NB; ++b)
                 if (see[b]) o[b][db][4 * x + e] += y;
             }
           }
@@ -460,9 +478,9 @@ __global__ __launch_bounds__(64 * kRowWaves, 2) void step_rows_kernel(const Step
 
   // ---- out
 #pragma unroll
-  for (int b = 0; b < 2; ++b) {
+  for (int b = 0; b < NB; ++b) {
     const float lt = l[b] + __shfl_xor(l[b], 32);
-    const int v0 = 64 * w + 32 * b, v = v0 + l32;
+    const int v0 = 32 * (NB * w + b), v = v0 + l32;
     const int n_vecs = it.n_rows * it.n_heads;
     const int n_mine = min(32, n_vecs - v0);
     if (n_mine <= 0) continue;
@@ -507,11 +525,19 @@ __global__ __launch_bounds__(64 * kRowWaves, 2) void step_rows_kernel(const Step
 }  // namespace
 
 hipError_t launch_step_rows(bool four_bit, const StepAttnArgs& a, int n_items, hipStream_t s) {
-  const dim3 grid(n_items), block(64 * kRowWaves);
-  if (four_bit)
-    hipLaunchKernelGGL(step_rows_kernel<true>, grid, block, 0, s, a);
+  const dim3 grid(n_items);
+#define TSR_ROWS(F4, NB) \
+  hipLaunchKernelGGL((step_rows_kernel<F4, NB>), grid, dim3(512 / NB), 0, s, a)
+  const bool alone = n_items <= kNumCus;   // a workgroup on each unit at most
+  if (four_bit && alone)
+    TSR_ROWS(true, 1);
+  else if (four_bit)
+    TSR_ROWS(true, 2);
+  else if (alone)
+    TSR_ROWS(false, 1);
   else
-    hipLaunchKernelGGL(step_rows_kernel<false>, grid, block, 0, s, a);
+    TSR_ROWS(false, 2);
+#undef TSR_ROWS
   return hipGetLastError();
 }
 

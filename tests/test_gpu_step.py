@@ -576,6 +576,78 @@ def test_four_bit_nan_block_reaches_only_its_rows(kernel):
     assert torch.isfinite(out[1:, :, :64]).all() and torch.isfinite(out[1:, :, 96:]).all()
 
 
+def copied(sess, reqs, q, **opt):
+    """The requests as often as the kernel for many rows needs for more work
+    items than a launch with a workgroup on each unit holds: outputs, [copies]
+    [rows][heads][d] and [copies][rows][heads]."""
+    opt = {"split_tiles": -1, **opt}   # automatic ranges go by the whole batch
+    one = sess.step(reqs, attn_kernel=2, **opt)
+    k = 256 // one.num_attn_items + 1
+    step = sess.step(list(reqs) * k, attn_kernel=2, **opt)
+    assert step.num_attn_items > 256 and step.attn_item_rows == 256
+    qk = q.repeat(k, 1, 1)
+    out = torch.full_like(qk, float("nan"))
+    lse = torch.full(qk.shape[:2], float("nan"), device="cuda")
+    sess.step_attn(step, qk, out, lse)
+    torch.cuda.synchronize()
+    return out.unflatten(0, (k, -1)), lse.unflatten(0, (k, -1))
+
+
+def same_bits(t):
+    """Every copy's bits are the first's."""
+    w = t.contiguous().view(torch.int16 if t.dtype == torch.bfloat16 else torch.int32)
+    return bool((w == w[:1]).all())
+
+
+@pytest.mark.parametrize("four_bit", [False, True])
+@pytest.mark.parametrize("name", ["one_key", "decode", "window_one", "window_sinks_meet", "lo",
+                                  "nothing", "nothing_cut", "cut_window", "g20", "page64", "many",
+                                  "many_window", "many_cut_window", "many_mha", "many_g5",
+                                  "many_spread", "many_lo", "many_nothing"])
+def test_full_launch(name, four_bit):
+    """More work items than units: the other form of the kernel for many rows."""
+    sh, lens, opt = CASES[name]
+    sh = shape(**sh)
+    reqs, n = batch(lens, sh.page_size, seed=len(name))
+    sess, _, q, _, _ = run_attn(sh, reqs, n, len(name), **opt)
+    kv = pages_kv(sess, reqs)
+    if four_bit:
+        bf = sess
+        sess = Session(sh, 1, n, four_bit=True)
+        sess.req_k.copy_(bf.req_k), sess.req_v.copy_(bf.req_v)
+        sess.req4_scale.fill_(255)
+        sess.req4_k.fill_(0x77), sess.req4_v.fill_(0x77)
+        sess.pack_step(sess.step(reqs, four_bit=True))
+        kv = four_bit_kv(sess, reqs)
+    out, lse = copied(sess, reqs, q, four_bit=four_bit, **opt)
+    check_attn(reqs, q, out[0], lse[0], kv, 128, max(r.kv_len for r in reqs),
+               opt.get("window", 0), opt.get("n_sinks", 0), part=FP16)
+    assert same_bits(out) and same_bits(lse)
+
+
+@pytest.mark.parametrize("split", [-1, 1])
+def test_unseen_values_stay_out_of_a_full_launch(split):
+    sh = shape(hq=4, hkv=1)
+    reqs, n = batch([(96, [40, 41, 70, 95], [0, 0, 10, 64]), (300, 140)], 16)
+    t = reqs[0].block_table
+
+    def poison(s):
+        for key, x in ((41, float("inf")), (70, float("nan")), (3, float("-inf"))):
+            s.req_v[0, t[key // 16], 0, key % 16, 5] = x
+        s.req_k[0, t[60 // 16], 0, 60 % 16, 1] = float("nan")
+        s.req_v[0, reqs[1].block_table[-1], 0, 11] = float("inf")   # key 299, the last row's own
+
+    opt = dict(split_tiles=split, window=25, n_sinks=2)
+    sess, _, q, out, lse = run_attn(sh, reqs, n, 5, poison=poison, attn_kernel=2, **opt)
+    many, mlse = copied(sess, reqs, q, **opt)
+    assert torch.isinf(out[-1]).all() and torch.isfinite(out[4:-1]).all()
+    for a, b in ((many, out), (mlse, lse)):
+        assert same_bits(a)
+        assert torch.equal(torch.isnan(a[0]), torch.isnan(b))
+        assert torch.equal(torch.isposinf(a[0]), torch.isposinf(b))
+        assert torch.equal(torch.isneginf(a[0]), torch.isneginf(b))
+
+
 # ------------------------------------------------- the operators as used
 def test_decode_after_composed_prefill():
     """A composed prefill, then tokens decoded over its pages: bf16, and from
