@@ -45,6 +45,8 @@ namespace {
 constexpr int kRowBytes = 2 * kD;   // a key's K or V row in LDS
 constexpr int kTileBytes = kStepKeys * kRowBytes;
 constexpr int kBlkBytes = 16 * kRowBytes;   // a 16-key block of either
+constexpr int kPartStr = 144;   // bytes for 32 dims of a partial row on its way out
+constexpr int kPartLds = 32 * kPartStr;
 
 // Fragments of a second block's queries that stay in LDS: with 16 in
 // registers the tile loop spills (its reloads would also wait for the direct
@@ -74,6 +76,7 @@ template <bool F4, int NB>
 __global__ __launch_bounds__(512 / NB, 2) void step_rows_kernel(const StepAttnArgs a) {
   constexpr int NW = 8 / NB, TG = NW / 2, QL = kQInLds<NB>;
   constexpr int kGroupBytes = TG * kTileBytes;
+  static_assert(NW * kPartLds <= 2 * kGroupBytes, "rows on their way out fit K's buffers");
   // two groups of tiles, K and V
   __shared__ __attribute__((aligned(1024))) uint8_t kl[2 * kGroupBytes];
   __shared__ __attribute__((aligned(1024))) uint8_t vl[2 * kGroupBytes];
@@ -489,16 +492,28 @@ __global__ __launch_bounds__(512 / NB, 2) void step_rows_kernel(const StepAttnAr
     if (it.part_slot >= 0) {
       const bool none = lt == 0.0f;
       const float inv = none ? 0.0f : 1.0f / lt;
-      if (v < n_vecs) {
-        const int64_t at = (int64_t)it.part_slot + v;
+      if (v < n_vecs && lh == 0)
+        a.split_lse[(int64_t)it.part_slot + v] = none ? -INFINITY : ls;
+      // through LDS, 32 dims at a time: a store writes 128 bytes of each of eight
+      // rows (from the registers, 32 bytes of 32)
+      uint8_t* rows = kl + w * kPartLds;
+      float* to = a.split_o + ((int64_t)it.part_slot + v0) * kD;
 #pragma unroll
-        for (int db = 0; db < 4; ++db)
+      for (int db = 0; db < 4; ++db) {
 #pragma unroll
-          for (int x = 0; x < 4; ++x)
-            *reinterpret_cast<float4*>(a.split_o + at * kD + 32 * db + 8 * x + 4 * lh) =
-                make_float4(o[b][db][4 * x] * inv, o[b][db][4 * x + 1] * inv,
-                            o[b][db][4 * x + 2] * inv, o[b][db][4 * x + 3] * inv);
-        if (lh == 0) a.split_lse[at] = none ? -INFINITY : ls;
+        for (int x = 0; x < 4; ++x)
+          *reinterpret_cast<f32x4*>(rows + l32 * kPartStr + 32 * x + 16 * lh) =
+              f32x4{o[b][db][4 * x] * inv, o[b][db][4 * x + 1] * inv, o[b][db][4 * x + 2] * inv,
+                    o[b][db][4 * x + 3] * inv};
+        // LDS keeps a wave's accesses in order; this keeps the compiler to it
+        asm volatile("" ::: "memory");
+#pragma unroll
+        for (int h = 0; h < 4; ++h) {
+          const int row = 8 * h + (lane >> 3), c = lane & 7;
+          const f32x4 y = *reinterpret_cast<const f32x4*>(rows + row * kPartStr + 16 * c);
+          if (row < n_mine) *reinterpret_cast<f32x4*>(to + row * kD + 32 * db + 4 * c) = y;
+        }
+        asm volatile("" ::: "memory");
       }
       continue;
     }
