@@ -164,6 +164,7 @@ CASES = {
     "cut": (dict(), [(1000, 1), (64, 1), (31, 2)], dict(split_tiles=1)),
     "cut_window": (dict(), [(999, 2), (450, 1)], dict(split_tiles=3, window=200, n_sinks=70)),
     "cut_odd": (dict(), [(2001, 1)], dict(split_tiles=7)),
+    "cut_pairs": (dict(), [(64, 3), (50, 1), (20, 1)], dict(split_tiles=1)),
     "mha": (dict(hq=4, hkv=4), [(60, 21), (130, 1)], dict(window=50, n_sinks=1)),
     "g3": (dict(hq=6, hkv=2), [(61, 7), (130, 1)], dict()),
     "g8": (dict(hq=16, hkv=2), [(45, 5), (200, 1)], dict(split_tiles=2)),
@@ -196,6 +197,8 @@ CASES = {
             dict(window=60, n_sinks=3)),
     "f32_page8": (dict(hq=6, hkv=2, kv="f32", page=8), [(50, 20), (1, 1)], dict()),
     "f32_256": (dict(hq=4, hkv=2, d=256, kv="f32"), [(70, 9)], dict(split_tiles=1)),
+    "f32_pairs": (dict(hq=4, hkv=2, kv="f32"), [(64, 3), (50, 1), (20, 1)],
+                  dict(split_tiles=1)),
     "f32_lo": (dict(hq=4, hkv=1, d=64, kv="f32"), [(90, [-1, 20, 89], [0, 21, 40])],
                dict(split_tiles=1, window=33, n_sinks=2)),
 }
